@@ -172,6 +172,76 @@ mote_status mote_router_balance(const void* x, const void* w_router, const float
                                 void* hip_stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Scored routing: the router of layers whose gate is not the plain softmax top-k of Eq.3.
+ *
+ *   l[t,e] = sum_c x[t,c] * w_router[c,e]                                  (fp64)
+ *   s      = softmax over all E logits, or sigmoid of each
+ *   key    = s + select_bias (fp64); the logits themselves where there is neither a bias nor a group score of
+ *            two keys (the same order, and none is lost where scores round to the same value)
+ *   groups : expert e belongs to group e / (E / n_groups); a group's score is the sum of its group_top largest
+ *            keys; only the experts of the top_groups best groups can be selected (ties to the lower group)
+ *   selection: the top_k largest keys in descending order, exact ties to the lower expert index
+ *   weight = scale * s_i, or with renormalise scale * s_i / sum over the selected of s (evaluated as a softmax over
+ *            log s of the selected: scores that underflow together still share the weight)
+ *
+ * The selection bias decides who is selected and has no part in the weights.  An expert whose key is -inf (a bias of -inf
+ * switches it off) is never selected: slots that find no expert get index -1 and weight 0.  A NaN key ranks as the lowest
+ * finite value: indices stay in range and the weights carry the NaN.  Indices follow from fp64 logits whatever kernel
+ * computes them: sums whose order could matter are settled in fp64 before an index is written.
+ *
+ * cfg          in : the description above; top_k <= 8 and at most the experts of top_groups groups, n_groups divides E,
+ *                   group_top 1 or 2 and at most E / n_groups.  n_groups == 1: no groups (top_groups, group_top 1)
+ * x            in : bf16 [T, d];   w_router in : bf16 [d, E]
+ * select_bias  in : fp32 [E] or NULL
+ * token_mask   in : uint8 [T] or NULL; a token whose byte is 0 is padding: indices -1, weights 0, not counted, not in
+ *                   the score sums
+ * topk_idx     out: int32 [T, top_k];   topk_w out: fp32 [T, top_k]
+ * logits       out: fp32 [T, E] or NULL (mote_route_backward reads them; written for padding too)
+ * expert_counts out: int32 [E] or NULL; number of (token, slot) pairs of each expert
+ * score_sum    out: fp32 [E] or NULL; sum over the tokens of s (fp64 sums in a fixed order): with expert_counts the two
+ *                   factors of Eq.12
+ * workspace       : device, >= mote_route_workspace_bytes(T, E), 256-byte aligned; may be NULL when expert_counts and
+ *                   score_sum are
+ * Limits: d % 128 == 0, 1 <= E <= 64, T * top_k < 2^24; T == 0 leaves counts and sums zero.
+ * Softmax without groups, bias and renormalise selects as mote_router_topk does (finite logits). */
+enum { MOTE_SCORE_SOFTMAX = 0, MOTE_SCORE_SIGMOID = 1 };
+typedef struct {
+  int score;        /* MOTE_SCORE_SOFTMAX or MOTE_SCORE_SIGMOID          */
+  int top_k;
+  int n_groups;     /* 1: every expert can be selected                   */
+  int top_groups;   /* groups a token may select from                    */
+  int group_top;    /* keys that make a group's score: 1 or 2            */
+  int renormalise;  /* 0: weights are scores, else they add up to scale  */
+  float scale;      /* finite                                            */
+} mote_routing;
+size_t mote_route_workspace_bytes(int T, int E);
+mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_router, const float* select_bias,
+                       const uint8_t* token_mask, int T, int d, int E, int32_t* topk_idx, float* topk_w, float* logits,
+                       int32_t* expert_counts, float* score_sum, void* workspace, size_t workspace_bytes,
+                       void* hip_stream);
+
+/* Gradients of mote_route through the weights and the score sums (the indices are constants):
+ *
+ *   dlogits = d(sum_tj d_topk_w[t,j] * topk_w[t,j] + sum_e d_score_sum[e] * score_sum[e]) / dlogits      (fp32)
+ *   dx[t,c] = sum_e dlogits[t,e] * w_router[c,e],     dw_router[c,e] = sum_t x[t,c] * dlogits[t,e]
+ *
+ * d_score_sum of Eq.12 with weight gamma is gamma * E / T * expert_counts (counts are constants there too).
+ * Operands of the two products are exact (fp32 dlogits as three bf16 terms against bf16 x and w_router), sums are fp32 in a
+ * fixed order.  A padding token (token_mask) has a zero gradient row; slots of index -1 have no part.
+ *
+ * cfg: score, top_k, renormalise and scale as in the forward call (groups and bias do not enter)
+ * logits in : fp32 [T, E] of the forward call;  topk_idx in : int32 [T, top_k];  d_topk_w in : fp32 [T, top_k]
+ * d_score_sum in : fp32 [E] or NULL;  token_mask in : uint8 [T] or NULL
+ * dx out : fp32 [T, d] or NULL;  dw_router out : fp32 [d, E] or NULL (zero for T == 0)
+ * workspace : device, >= mote_route_backward_workspace_bytes(T, d, E), 256-byte aligned
+ * Limits as mote_route; indices outside 0 .. E - 1 count as -1, one expert twice in a row counts twice. */
+size_t mote_route_backward_workspace_bytes(int T, int d, int E);
+mote_status mote_route_backward(const mote_routing* cfg, const void* x, const void* w_router, const float* logits,
+                                const int32_t* topk_idx, const float* d_topk_w, const float* d_score_sum,
+                                const uint8_t* token_mask, int T, int d, int E, float* dx, float* dw_router,
+                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------
  * Whole layer.
  */
 typedef struct {
@@ -271,6 +341,82 @@ mote_status mote_block_forward(const mote_layer* layer, const mote_norm* norm, c
 #define MOTE_STATIC_WORKSPACE_BYTES (64u << 20)
 mote_status mote_layer_forward_static(const mote_layer* layer, const void* x, int T, void* out,
                                       const mote_taps* taps, void* hip_stream);
+
+/* mote_layer_forward on a routing that the caller has, of mote_route or of a scheme of its own, in the place of the
+ * layer's router (w_router and router_bias are not read and may be NULL).
+ * topk_idx in : int32 [T, k], k = layer->top_k;  topk_w in : fp32 [T, k]
+ * A slot whose index is outside 0 .. E - 1 adds nothing to its token (its row is computed, with weight 0, as one of expert
+ * 0); an expert twice in a row adds twice.  Everything else, workspace and limits included, as in mote_layer_forward;
+ * taps->topk_idx and topk_p are the routing as it was used. */
+mote_status mote_layer_forward_routed(const mote_layer* layer, const void* x, int T, const int32_t* topk_idx,
+                                      const float* topk_w, void* out, void* workspace, size_t workspace_bytes,
+                                      const mote_taps* taps, void* hip_stream);
+
+/* The residual stream between two branches of a block: the norm behind a branch, its gate, the scaled residual sum and
+ * the norm in front of the next branch, in one pass.
+ *
+ *   z      = N_post(y)                                       (post == NULL: z = y)
+ *   total  = residual_scale * r + branch_scale * gate * z    (gate == NULL: 1; per channel)
+ *   normed = N_pre(total)                                    (pre == NULL: not written)
+ *
+ * N is the norm of mote_block_forward.  Everything between the loads and the two stores is fp32 (row sums included); normed
+ * is taken from the sum before its rounding.
+ * dtype        : MOTE_DTYPE_BF16 or MOTE_DTYPE_F32, of r, y, total, normed and their gradients; gamma, beta, gate: bf16 [d]
+ * r, y     in  : [T, d];   total, normed out : [T, d]
+ * Limits: d % 8 == 0, 8 <= d <= 8192; eps >= 0, scales finite.  T == 0 is a no-op. */
+typedef struct {
+  const mote_norm* post;
+  const void* gate;
+  float residual_scale, branch_scale;
+  const mote_norm* pre;
+} mote_residual;
+mote_status mote_residual_norm(const mote_residual* block, const void* r, const void* y, int dtype, int T, int d,
+                               void* total, void* normed, void* hip_stream);
+
+/* Gradients of mote_residual_norm for the gradients d_total and d_normed of its outputs (either may be NULL: zero; d_normed
+ * must be NULL without a pre norm).  Row quantities are computed again from r and y in fp32.
+ * dr, dy   out : [T, d] of `dtype`, rounded once
+ * parameter gradients out: fp32 [d], sums over the rows in a fixed order, zero for T == 0; each may be NULL, and those of
+ * parameters that the block does not have are not written
+ * workspace    : device, >= mote_residual_norm_workspace_bytes(block, T, d), 256-byte aligned */
+typedef struct {
+  float* gate;
+  float* post_gamma;
+  float* post_beta;
+  float* pre_gamma;
+  float* pre_beta;
+} mote_residual_grads;
+size_t mote_residual_norm_workspace_bytes(const mote_residual* block, int T, int d);
+mote_status mote_residual_norm_backward(const mote_residual* block, const void* r, const void* y, const void* d_total,
+                                        const void* d_normed, int dtype, int T, int d, void* dr, void* dy,
+                                        const mote_residual_grads* grads, void* workspace, size_t workspace_bytes,
+                                        void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Clipping by the global norm of many gradient tensors (the dW of mote_ste_linear_backward and mote_route_backward, the
+ * parameter gradients of the norms, ...).
+ *
+ *   norm = sqrt(sum over all tensors and elements of g^2)        (fp64 sums in a fixed order)
+ *   out  = g * c (fp64, rounded to fp32 and then to the type), c = max_norm / norm where norm > max_norm, else 1
+ *
+ * A norm that is not finite leaves the values as they are (c = 1) and is reported, so that the caller can skip the step.
+ * grads_host in : HOST array of n descriptors, read before the call returns.  out == NULL or out == grad: in place, not
+ *                 written where c == 1.  Tensors of zero elements are allowed.  Pointers need the alignment of their type
+ *                 only (16 bytes are faster).  No two outputs may overlap, nor an output another tensor's gradient: such a
+ *                 list is refused with MOTE_ERR_INVALID_ARG.
+ * max_norm       : > 0; +inf only measures
+ * norm       out : device fp32 [1]
+ * workspace      : device, >= mote_clip_grad_norm_workspace_bytes(n), 256-byte aligned
+ * Limits: 0 <= n <= 4096, below 2^40 elements a tensor and 2^44 in all. */
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t n;
+  int dtype;   /* MOTE_DTYPE_F32 or MOTE_DTYPE_BF16, of grad and out */
+} mote_grad;
+size_t mote_clip_grad_norm_workspace_bytes(int n_tensors);
+mote_status mote_clip_grad_norm(const mote_grad* grads_host, int n_tensors, float max_norm, float* norm, void* workspace,
+                                size_t workspace_bytes, void* hip_stream);
 
 /* ---------------------------------------------------------------------------------------
  * Measurement support (not part of the layer's mathematics).

@@ -493,3 +493,158 @@ def block_forward(x_a_bf16, norm, w_router_bf16, bias, k, shared, experts, token
     blk = bf16_to_f32(x_a_bf16[out["tokens"]]).astype(np.float64) + out["out_f64"]
     out.update(xn=xn, block_f32=blk.astype(np.float32), block_bf16=f32_to_bf16(blk.astype(np.float32)))
     return out
+
+
+# ------------------------------------------------------- operators of a training step around the layer
+# Plain fp64 definitions on real-valued arrays (callers convert bf16 bits with bf16_to_f32).
+def _scores(logits: np.ndarray, score: str) -> np.ndarray:
+    with np.errstate(over="ignore", invalid="ignore"):
+        if score == "sigmoid":
+            return 1.0 / (1.0 + np.exp(-logits))
+        e = np.exp(logits - logits.max(axis=1, keepdims=True))
+        return e / e.sum(axis=1, keepdims=True)
+
+
+def _log_scores(logits: np.ndarray, score: str) -> np.ndarray:
+    if score == "sigmoid":
+        return np.minimum(logits, 0.0) - np.log1p(np.exp(-np.abs(logits)))
+    return logits - logits.max(axis=1, keepdims=True)      # up to a constant of the row
+
+
+def _slot_weights(logits, idx, score, renormalise):
+    """Weight of every slot (0 where idx is -1), before the scale."""
+    there = idx >= 0
+    at = np.where(there, idx, 0)
+    if not renormalise:
+        return np.where(there, np.take_along_axis(_scores(logits, score), at, 1), 0.0)
+    a = np.where(there, np.take_along_axis(_log_scores(logits, score), at, 1), -np.inf)
+    top = np.where(there.any(1), a.max(axis=1, initial=-np.inf), 0.0)
+    e = np.exp(a - top[:, None])
+    s = e.sum(axis=1, keepdims=True)
+    return np.divide(e, s, out=np.zeros_like(e), where=s != 0)
+
+
+def route(x, w_router, top_k, score="softmax", select_bias=None, token_mask=None, n_groups=1, top_groups=1, group_top=1,
+          renormalise=False, scale=1.0):
+    """Scored routing: loops over tokens and groups.  Returns dict(idx int32 [T, k], w, logits, scores, counts, score_sum)."""
+    with np.errstate(invalid="ignore", over="ignore"):
+        logits = np.asarray(x, np.float64) @ np.asarray(w_router, np.float64)
+    n_tok, n_exp = logits.shape
+    scores = _scores(logits, score)
+    use_logits = select_bias is None and not (n_groups > 1 and group_top == 2)
+    keys = logits.copy() if use_logits else scores + (0.0 if select_bias is None else np.asarray(select_bias, np.float32).astype(np.float64))
+    keys = np.where(np.isnan(keys), -np.finfo(np.float64).max, keys)
+    idx = np.full((n_tok, top_k), -1, np.int32)
+    live = np.ones(n_tok, bool) if token_mask is None else np.asarray(token_mask) != 0
+    per = n_exp // n_groups
+    for t in np.flatnonzero(live):
+        allowed = range(n_exp)
+        if n_groups > 1:
+            with np.errstate(over="ignore"):
+                best = [sum(sorted(keys[t, g * per:(g + 1) * per])[::-1][:group_top]) for g in range(n_groups)]
+            groups = sorted(range(n_groups), key=lambda g: (-best[g], g))[:top_groups]
+            allowed = [e for g in groups for e in range(g * per, (g + 1) * per)]
+        order = sorted((e for e in allowed if keys[t, e] > -np.inf), key=lambda e: (-keys[t, e], e))[:top_k]
+        idx[t, :len(order)] = order
+    w = _slot_weights(logits, idx, score, renormalise) * float(np.float32(scale))
+    counts = np.array([(idx == e).sum() for e in range(n_exp)], np.int32)
+    return dict(idx=idx, w=w, logits=logits, scores=scores, counts=counts, score_sum=scores[live].sum(axis=0), keys=keys)
+
+
+def route_loss(logits, idx, d_w, d_score_sum, token_mask, score, renormalise, scale):
+    """The scalar whose gradient route_backward takes: sum d_w * w + sum d_score_sum * score_sum."""
+    live = np.ones(len(logits), bool) if token_mask is None else np.asarray(token_mask) != 0
+    w = _slot_weights(logits, np.where(live[:, None], idx, -1), score, renormalise) * scale
+    loss = float((w * d_w).sum())
+    if d_score_sum is not None:
+        loss += float((_scores(logits, score)[live].sum(axis=0) * d_score_sum).sum())
+    return loss
+
+
+def route_backward(x, w_router, logits, idx, d_w, d_score_sum=None, token_mask=None, score="softmax", renormalise=False, scale=1.0):
+    """(dlogits, dx, dw, magnitude) with magnitude the same sum as dlogits over absolute values."""
+    logits, d_w = np.asarray(logits, np.float64), np.asarray(d_w, np.float64)
+    n_tok, n_exp = logits.shape
+    s = _scores(logits, score)
+    other = _scores(-logits, "sigmoid") if score == "sigmoid" else np.ones_like(s)
+    q = np.zeros(n_exp) if d_score_sum is None else np.asarray(d_score_sum, np.float64)
+    g, mag = np.zeros_like(s), np.zeros_like(s)
+    w = _slot_weights(logits, idx, score, renormalise)
+    for t in range(n_tok):
+        if token_mask is not None and not token_mask[t]:
+            continue
+        for j, e in enumerate(idx[t]):
+            if e < 0:
+                continue
+            if renormalise:                                  # d w_j / d a_i = w_j (delta - w_i) over the slots
+                for i, e2 in enumerate(idx[t]):
+                    if e2 >= 0:
+                        v = scale * d_w[t, j] * w[t, j] * ((i == j) - w[t, i])
+                        g[t, e2] += v * other[t, e2]
+                        mag[t, e2] += abs(scale * d_w[t, j] * w[t, j]) * ((i == j) + w[t, i]) * other[t, e2]
+            elif score == "sigmoid":
+                g[t, e] += scale * d_w[t, j] * s[t, e] * other[t, e]
+                mag[t, e] += abs(scale * d_w[t, j]) * s[t, e] * other[t, e]
+            else:
+                delta = np.arange(n_exp) == e
+                g[t] += scale * d_w[t, j] * s[t, e] * (delta - s[t])
+                mag[t] += abs(scale * d_w[t, j]) * s[t, e] * (delta + s[t])
+        if score == "sigmoid":
+            g[t] += s[t] * other[t] * q
+            mag[t] += s[t] * other[t] * np.abs(q)
+        else:
+            g[t] += s[t] * (q - (s[t] * q).sum())
+            mag[t] += s[t] * (np.abs(q) + (s[t] * np.abs(q)).sum())
+    return g, g @ np.asarray(w_router, np.float64).T, np.asarray(x, np.float64).T @ g, mag
+
+
+def _norm_parts(v, norm):
+    """norm: None or (kind, gamma, beta or None, eps).  Returns (output, hat, 1 / sqrt(var + eps))."""
+    if norm is None:
+        return v, v, np.ones((len(v), 1))
+    kind, gamma, beta, eps = norm
+    c = v - v.mean(axis=1, keepdims=True) if kind == "layer" else v
+    inv = 1.0 / np.sqrt((c * c).mean(axis=1, keepdims=True) + eps)
+    return c * inv * gamma + (beta if kind == "layer" else 0.0), c * inv, inv
+
+
+def residual_norm(r, y, post=None, gate=None, pre=None, residual_scale=1.0, branch_scale=1.0):
+    """(total, normed): total = a r + b gate N_post(y), normed = N_pre(total); norms as in _norm_parts."""
+    z = _norm_parts(y, post)[0]
+    total = residual_scale * r + branch_scale * (z if gate is None else gate * z)
+    return total, _norm_parts(total, pre)[0]
+
+
+def _norm_back(norm, hat, inv, up):
+    """Gradient of a norm's output: (input, gamma, beta)."""
+    if norm is None:
+        return up, None, None
+    u = up * norm[1]
+    d_in = u - hat * (u * hat).mean(axis=1, keepdims=True)
+    if norm[0] == "layer":
+        d_in = d_in - u.mean(axis=1, keepdims=True)
+    return inv * d_in, (up * hat).sum(axis=0), up.sum(axis=0) if norm[0] == "layer" else None
+
+
+def residual_norm_backward(r, y, d_total, d_normed, post=None, gate=None, pre=None, residual_scale=1.0, branch_scale=1.0):
+    """dict(dr, dy, gate, post_gamma, post_beta, pre_gamma, pre_beta); None where the block has no such parameter."""
+    z, hat_y, inv_y = _norm_parts(y, post)
+    total = residual_scale * r + branch_scale * (z if gate is None else gate * z)
+    _, hat, inv = _norm_parts(total, pre)
+    d_sum = np.zeros_like(r) if d_total is None else d_total.copy()
+    out = dict(pre_gamma=None, pre_beta=None)
+    if pre is not None:
+        d_in, out["pre_gamma"], out["pre_beta"] = _norm_back(pre, hat, inv, np.zeros_like(r) if d_normed is None else d_normed)
+        d_sum += d_in
+    d_b = branch_scale * d_sum
+    out["gate"] = None if gate is None else (d_b * z).sum(axis=0)
+    out["dy"], out["post_gamma"], out["post_beta"] = _norm_back(post, hat_y, inv_y, d_b if gate is None else d_b * gate)
+    out["dr"] = residual_scale * d_sum
+    return out
+
+
+def clip_grad_norm(grads, max_norm):
+    """(norm, scaled gradients) in fp64; a norm that is not finite leaves the gradients as they are."""
+    norm = float(np.sqrt(sum((np.asarray(g, np.float64) ** 2).sum() for g in grads)))
+    c = max_norm / norm if np.isfinite(norm) and norm > max_norm else 1.0
+    return norm, [np.asarray(g, np.float64) * c for g in grads]

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 from ctypes import POINTER, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -23,6 +24,9 @@ EXPORTS = ("mote_status_string", "mote_version", "mote_packed_bytes", "mote_pack
            "mote_router_topk", "mote_layer_workspace_bytes", "mote_layer_forward", "mote_layer_forward_static",
            "mote_block_forward", "mote_router_balance", "mote_pack_binary", "mote_rtn_packed_bytes", "mote_pack_rtn",
            "mote_ste_backward_workspace_bytes", "mote_ste_linear_backward",
+           "mote_route_workspace_bytes", "mote_route", "mote_route_backward_workspace_bytes", "mote_route_backward",
+           "mote_layer_forward_routed", "mote_residual_norm", "mote_residual_norm_workspace_bytes",
+           "mote_residual_norm_backward", "mote_clip_grad_norm_workspace_bytes", "mote_clip_grad_norm",
            "mote_stage_timing", "mote_stage_times", "mote_event_pair_overhead", "mote_tuning_set", "mote_calib_copy")
 KNOBS = ("no_fork", "fork_min_log2", "event_fence", "quant_wide", "routed_variant", "routed_down_variant",
          "shared_variant", "group_m", "dynamic_rounds", "decode_variant", "router_token_blocks", "down_split_tiles",
@@ -48,6 +52,24 @@ class MoteNormStruct(ctypes.Structure):
 
 
 NORM_RMS, NORM_LAYER = 1, 2
+
+
+class MoteRoutingStruct(ctypes.Structure):
+    _fields_ = [("score", c_int), ("top_k", c_int), ("n_groups", c_int), ("top_groups", c_int), ("group_top", c_int),
+                ("renormalise", c_int), ("scale", c_float)]
+
+
+class MoteResidualStruct(ctypes.Structure):
+    _fields_ = [("post", POINTER(MoteNormStruct)), ("gate", c_void_p), ("residual_scale", c_float), ("branch_scale", c_float),
+                ("pre", POINTER(MoteNormStruct))]
+
+
+class MoteResidualGradsStruct(ctypes.Structure):
+    _fields_ = [(name, c_void_p) for name in ("gate", "post_gamma", "post_beta", "pre_gamma", "pre_beta")]
+
+
+class MoteGradStruct(ctypes.Structure):
+    _fields_ = [("grad", c_void_p), ("out", c_void_p), ("n", c_int64), ("dtype", c_int)]
 
 
 TAP_FIELDS = ("topk_idx", "topk_p", "counts", "row_of", "tok_of", "q_x", "beta_x", "acc_gate",
@@ -106,6 +128,32 @@ def load_library() -> ctypes.CDLL:
     lib.mote_ste_linear_backward.argtypes = [c_void_p, POINTER(ctypes.c_int32), c_void_p, c_void_p, c_int, c_void_p,
                                              c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p,
                                              c_size_t, c_void_p]
+    lib.mote_route_workspace_bytes.restype = c_size_t
+    lib.mote_route_workspace_bytes.argtypes = [c_int, c_int]
+    lib.mote_route.restype = c_int
+    lib.mote_route.argtypes = [POINTER(MoteRoutingStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
+                               c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.mote_route_backward_workspace_bytes.restype = c_size_t
+    lib.mote_route_backward_workspace_bytes.argtypes = [c_int, c_int, c_int]
+    lib.mote_route_backward.restype = c_int
+    lib.mote_route_backward.argtypes = [POINTER(MoteRoutingStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.mote_layer_forward_routed.restype = c_int
+    lib.mote_layer_forward_routed.argtypes = [POINTER(MoteLayerStruct), c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                                              c_size_t, POINTER(MoteTapsStruct), c_void_p]
+    lib.mote_residual_norm.restype = c_int
+    lib.mote_residual_norm.argtypes = [POINTER(MoteResidualStruct), c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p,
+                                       c_void_p]
+    lib.mote_residual_norm_workspace_bytes.restype = c_size_t
+    lib.mote_residual_norm_workspace_bytes.argtypes = [POINTER(MoteResidualStruct), c_int, c_int]
+    lib.mote_residual_norm_backward.restype = c_int
+    lib.mote_residual_norm_backward.argtypes = [POINTER(MoteResidualStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int,
+                                                c_int, c_void_p, c_void_p, POINTER(MoteResidualGradsStruct), c_void_p, c_size_t,
+                                                c_void_p]
+    lib.mote_clip_grad_norm_workspace_bytes.restype = c_size_t
+    lib.mote_clip_grad_norm_workspace_bytes.argtypes = [c_int]
+    lib.mote_clip_grad_norm.restype = c_int
+    lib.mote_clip_grad_norm.argtypes = [POINTER(MoteGradStruct), c_int, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.mote_stage_timing.restype = c_int
     lib.mote_stage_timing.argtypes = [c_int]
     lib.mote_stage_times.restype = c_int
@@ -394,6 +442,267 @@ def mote_layer_forward_static(layer: MoteLayer, x: torch.Tensor, out: torch.Tens
                                          ctypes.byref(ts) if ts is not None else None, _stream()),
            "mote_layer_forward_static")
     return out
+
+
+class _on_device:
+    """The device of the given tensors (all on one) as the current one for a library call, whatever the caller's is."""
+
+    def __init__(self, **tensors):
+        dev = None
+        for name, t in tensors.items():
+            if t is None:
+                continue
+            dev = t.device if dev is None else dev
+            if t.device != dev:
+                raise MoteError(f"{name} is on {t.device}, the other tensors are on {dev}")
+        self._guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def _shape(t: torch.Tensor, shape, name: str) -> torch.Tensor:
+    if tuple(t.shape) != tuple(shape):
+        raise MoteError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return t
+
+
+def _workspace(given, need: int, device) -> torch.Tensor:
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=device) if given is None else _dev(given, torch.uint8, "workspace")
+
+
+def mote_layer_forward_routed(layer: MoteLayer, x: torch.Tensor, topk_idx: torch.Tensor, topk_w: torch.Tensor,
+                              out: torch.Tensor = None, taps: dict = None, workspace: torch.Tensor = None) -> torch.Tensor:
+    """mote_layer_forward on a given routing (topk_idx int32, topk_w fp32 [T, k], e.g. of mote_route) instead of the layer's
+    router; a slot whose index is outside 0 .. E - 1 adds nothing."""
+    lib = load_library()
+    _dev(x, torch.bfloat16, "x")
+    n_tok = x.shape[0]
+    _shape(x, (n_tok, layer.d_model), "x")
+    _shape(_dev(topk_idx, torch.int32, "topk_idx"), (n_tok, layer.top_k), "topk_idx")
+    _shape(_dev(topk_w, torch.float32, "topk_w"), (n_tok, layer.top_k), "topk_w")
+    if out is None:
+        out = torch.empty_like(x)
+    _shape(_dev(out, torch.bfloat16, "out"), x.shape, "out")
+    with _on_device(x=x, topk_idx=topk_idx, topk_w=topk_w, out=out, w_router=layer.tensors["w_router"], workspace=workspace):
+        if workspace is None:
+            workspace = layer.workspace(max(n_tok, 1))
+        ts = None
+        if taps is not None:
+            ts = MoteTapsStruct(*[taps[n].data_ptr() if n in taps else None for n in TAP_FIELDS])
+        _check(lib.mote_layer_forward_routed(ctypes.byref(layer.struct), _ptr(x), n_tok, _ptr(topk_idx), _ptr(topk_w), _ptr(out),
+                                             _ptr(workspace), workspace.numel(), ctypes.byref(ts) if ts is not None else None,
+                                             _stream()), "mote_layer_forward_routed")
+    return out
+
+
+SCORES = ("softmax", "sigmoid")
+
+
+class MoteRouting:
+    """How mote_route scores and selects (include/mote.h, mote_routing)."""
+
+    def __init__(self, top_k: int, score: str = "softmax", n_groups: int = 1, top_groups: int = 1, group_top: int = 1,
+                 renormalise: bool = False, scale: float = 1.0):
+        if score not in SCORES:
+            raise MoteError(f"score must be one of {SCORES}, got {score!r}")
+        self.top_k = int(top_k)
+        self.struct = MoteRoutingStruct(SCORES.index(score), self.top_k, n_groups, top_groups, group_top, 1 if renormalise else 0, scale)
+
+
+class Routed(NamedTuple):
+    """Result of mote_route; logits, counts and score_sum are None unless asked for."""
+    topk_idx: torch.Tensor    # int32 [T, k], -1: no expert
+    topk_w: torch.Tensor      # fp32 [T, k]
+    logits: Optional[torch.Tensor]      # fp32 [T, E]
+    counts: Optional[torch.Tensor]      # int32 [E]
+    score_sum: Optional[torch.Tensor]   # fp32 [E]
+
+
+def _router_operands(x, w_router, token_mask):
+    _dev(x, torch.bfloat16, "x")
+    _dev(w_router, torch.bfloat16, "w_router")
+    if x.dim() != 2 or w_router.dim() != 2 or w_router.shape[0] != x.shape[1]:
+        raise MoteError(f"x {list(x.shape)} and w_router {list(w_router.shape)} do not fit: [T, d] and [d, E]")
+    if token_mask is not None:
+        if token_mask.dtype == torch.bool:
+            token_mask = token_mask.view(torch.uint8)
+        _shape(_dev(token_mask, torch.uint8, "token_mask"), (x.shape[0],), "token_mask")
+    return x.shape[0], x.shape[1], w_router.shape[1], token_mask
+
+
+def mote_route(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRouting, select_bias: torch.Tensor = None,
+               token_mask: torch.Tensor = None, want_logits: bool = False, want_stats: bool = False,
+               workspace: torch.Tensor = None) -> Routed:
+    """Scored routing of x bf16 [T, d] by w_router bf16 [d, E]; select_bias fp32 [E], token_mask bool or uint8 [T] (0: padding)."""
+    lib = load_library()
+    n_tok, d, n_exp, token_mask = _router_operands(x, w_router, token_mask)
+    if select_bias is not None:
+        _shape(_dev(select_bias, torch.float32, "select_bias"), (n_exp,), "select_bias")
+    with _on_device(x=x, w_router=w_router, select_bias=select_bias, token_mask=token_mask, workspace=workspace):
+        dev, k = x.device, routing.top_k
+        idx = torch.empty(n_tok, k, dtype=torch.int32, device=dev)
+        wt = torch.empty(n_tok, k, dtype=torch.float32, device=dev)
+        logits = torch.empty(n_tok, n_exp, dtype=torch.float32, device=dev) if want_logits else None
+        counts = score_sum = None
+        if want_stats:
+            counts = torch.empty(n_exp, dtype=torch.int32, device=dev)
+            score_sum = torch.empty(n_exp, dtype=torch.float32, device=dev)
+            workspace = _workspace(workspace, lib.mote_route_workspace_bytes(n_tok, n_exp), dev)
+        _check(lib.mote_route(ctypes.byref(routing.struct), _ptr(x), _ptr(w_router), _ptr(select_bias), _ptr(token_mask), n_tok, d,
+                              n_exp, _ptr(idx), _ptr(wt), _ptr(logits), _ptr(counts), _ptr(score_sum), _ptr(workspace),
+                              workspace.numel() if workspace is not None else 0, _stream()), "mote_route")
+    return Routed(idx, wt, logits, counts, score_sum)
+
+
+def mote_route_backward(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRouting, logits: torch.Tensor,
+                        topk_idx: torch.Tensor, d_topk_w: torch.Tensor, d_score_sum: torch.Tensor = None,
+                        token_mask: torch.Tensor = None, want_dx: bool = True, want_dw: bool = True,
+                        workspace: torch.Tensor = None):
+    """Gradients of mote_route: (dx fp32 [T, d], dw_router fp32 [d, E]) for d_topk_w fp32 [T, k] and d_score_sum fp32 [E]."""
+    lib = load_library()
+    n_tok, d, n_exp, token_mask = _router_operands(x, w_router, token_mask)
+    _shape(_dev(logits, torch.float32, "logits"), (n_tok, n_exp), "logits")
+    _shape(_dev(topk_idx, torch.int32, "topk_idx"), (n_tok, routing.top_k), "topk_idx")
+    _shape(_dev(d_topk_w, torch.float32, "d_topk_w"), (n_tok, routing.top_k), "d_topk_w")
+    if d_score_sum is not None:
+        _shape(_dev(d_score_sum, torch.float32, "d_score_sum"), (n_exp,), "d_score_sum")
+    with _on_device(x=x, w_router=w_router, logits=logits, topk_idx=topk_idx, d_topk_w=d_topk_w, d_score_sum=d_score_sum,
+                    token_mask=token_mask, workspace=workspace):
+        dev = x.device
+        dx = torch.empty(n_tok, d, dtype=torch.float32, device=dev) if want_dx else None
+        dw = torch.empty(d, n_exp, dtype=torch.float32, device=dev) if want_dw else None
+        workspace = _workspace(workspace, lib.mote_route_backward_workspace_bytes(n_tok, d, n_exp), dev)
+        _check(lib.mote_route_backward(ctypes.byref(routing.struct), _ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx),
+                                       _ptr(d_topk_w), _ptr(d_score_sum), _ptr(token_mask), n_tok, d, n_exp, _ptr(dx), _ptr(dw),
+                                       _ptr(workspace), workspace.numel(), _stream()), "mote_route_backward")
+    return dx, dw
+
+
+class MoteNorm:
+    """A norm of mote_block_forward's kinds: RMSNorm when beta is None, else layer normalisation; gamma, beta bf16 [d]."""
+
+    def __init__(self, gamma: torch.Tensor, beta: torch.Tensor = None, eps: float = 1e-6):
+        self.gamma = _dev(gamma, torch.bfloat16, "gamma")
+        self.beta = None if beta is None else _shape(_dev(beta, torch.bfloat16, "beta"), gamma.shape, "beta")
+        self.struct = MoteNormStruct(NORM_RMS if beta is None else NORM_LAYER, gamma.data_ptr(),
+                                     beta.data_ptr() if beta is not None else None, float(eps))
+
+
+class MoteResidual:
+    """total = residual_scale * r + branch_scale * gate * post(y), normed = pre(total); post, pre: MoteNorm or None, gate
+    bf16 [d] or None.  Holds the parameter tensors and the C struct that points at them."""
+
+    def __init__(self, d: int, post: MoteNorm = None, gate: torch.Tensor = None, pre: MoteNorm = None,
+                 residual_scale: float = 1.0, branch_scale: float = 1.0):
+        self.d, self.post, self.gate, self.pre = int(d), post, gate, pre
+        for name, t in (("post gamma", post and post.gamma), ("gate", gate), ("pre gamma", pre and pre.gamma)):
+            if t is not None:
+                _shape(_dev(t, torch.bfloat16, name), (self.d,), name)
+        self.struct = MoteResidualStruct(ctypes.pointer(post.struct) if post is not None else None,
+                                         gate.data_ptr() if gate is not None else None, residual_scale, branch_scale,
+                                         ctypes.pointer(pre.struct) if pre is not None else None)
+
+    def _tensors(self):
+        return dict(post_gamma=self.post and self.post.gamma, gate=self.gate, pre_gamma=self.pre and self.pre.gamma)
+
+
+def _residual_operands(block: MoteResidual, **tensors):
+    dtype = next(iter(tensors.values())).dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise MoteError(f"activations must be fp32 or bf16, got {dtype}")
+    n_tok = next(iter(tensors.values())).shape[0]
+    for name, t in tensors.items():
+        if t is not None:
+            _shape(_dev(t, dtype, name), (n_tok, block.d), name)
+    return n_tok, MOTE_DTYPE_F32 if dtype == torch.float32 else MOTE_DTYPE_BF16
+
+
+def mote_residual_norm(block: MoteResidual, r: torch.Tensor, y: torch.Tensor, total: torch.Tensor = None,
+                       normed: torch.Tensor = None):
+    """(total, normed) of the residual stream r and the branch output y, bf16 or fp32 [T, d]; normed is None without a pre norm."""
+    lib = load_library()
+    if block.pre is None and normed is not None:
+        raise MoteError("normed needs a block with a pre norm")
+    n_tok, dt = _residual_operands(block, r=r, y=y, total=total, normed=normed)
+    with _on_device(r=r, y=y, total=total, normed=normed, **block._tensors()):
+        total = torch.empty_like(r) if total is None else total
+        if normed is None and block.pre is not None:
+            normed = torch.empty_like(r)
+        _check(lib.mote_residual_norm(ctypes.byref(block.struct), _ptr(r), _ptr(y), dt, n_tok, block.d, _ptr(total), _ptr(normed),
+                                      _stream()), "mote_residual_norm")
+    return total, normed
+
+
+class ResidualGrads(NamedTuple):
+    """Gradients of mote_residual_norm: of r and y in their type, of the parameters in fp32 [d] (None: the block has none)."""
+    dr: torch.Tensor
+    dy: torch.Tensor
+    gate: Optional[torch.Tensor]
+    post_gamma: Optional[torch.Tensor]
+    post_beta: Optional[torch.Tensor]
+    pre_gamma: Optional[torch.Tensor]
+    pre_beta: Optional[torch.Tensor]
+
+
+def mote_residual_norm_backward(block: MoteResidual, r: torch.Tensor, y: torch.Tensor, d_total: torch.Tensor = None,
+                                d_normed: torch.Tensor = None, want_params: bool = True,
+                                workspace: torch.Tensor = None) -> ResidualGrads:
+    """Gradients of mote_residual_norm(block, r, y) for the gradients of its outputs (None: zero)."""
+    lib = load_library()
+    n_tok, dt = _residual_operands(block, r=r, y=y, d_total=d_total, d_normed=d_normed)
+    with _on_device(r=r, y=y, d_total=d_total, d_normed=d_normed, workspace=workspace, **block._tensors()):
+        dev = r.device
+        dr, dy = torch.empty_like(r), torch.empty_like(y)
+        has = (block.gate is not None, block.post is not None, block.post is not None and block.post.beta is not None,
+               block.pre is not None, block.pre is not None and block.pre.beta is not None)
+        par = [torch.empty(block.d, dtype=torch.float32, device=dev) if h and want_params else None for h in has]
+        workspace = _workspace(workspace, lib.mote_residual_norm_workspace_bytes(ctypes.byref(block.struct), n_tok, block.d), dev)
+        grads = MoteResidualGradsStruct(*[p.data_ptr() if p is not None else None for p in par])
+        _check(lib.mote_residual_norm_backward(ctypes.byref(block.struct), _ptr(r), _ptr(y), _ptr(d_total), _ptr(d_normed), dt, n_tok,
+                                               block.d, _ptr(dr), _ptr(dy), ctypes.byref(grads), _ptr(workspace),
+                                               workspace.numel(), _stream()), "mote_residual_norm_backward")
+    return ResidualGrads(dr, dy, *par)
+
+
+class GradClip:
+    """The list of gradients (contiguous fp32 or bf16 device tensors of one device) that mote_clip_grad_norm measures and
+    scales, in place or into `outs` (one per gradient, None: in place), with its descriptors and workspace."""
+
+    def __init__(self, grads, outs=None):
+        self.grads = list(grads)
+        self.outs = [None] * len(self.grads) if outs is None else list(outs)
+        if not self.grads or len(self.outs) != len(self.grads):
+            raise MoteError("GradClip needs at least one gradient, and as many outputs as gradients")
+        self.descriptors = (MoteGradStruct * len(self.grads))()
+        for s, g, o in zip(self.descriptors, self.grads, self.outs):
+            if g.dtype not in (torch.float32, torch.bfloat16):
+                raise MoteError(f"gradients must be fp32 or bf16, got {g.dtype}")
+            _dev(g, g.dtype, "gradient")
+            if o is not None:
+                _shape(_dev(o, g.dtype, "output"), g.shape, "output")
+            if g.device != self.grads[0].device or (o is not None and o.device != g.device):
+                raise MoteError("all gradients and outputs must be on one device")
+            s.grad, s.out, s.n = g.data_ptr(), o.data_ptr() if o is not None else None, g.numel()
+            s.dtype = MOTE_DTYPE_F32 if g.dtype == torch.float32 else MOTE_DTYPE_BF16
+        self.workspace = _workspace(None, load_library().mote_clip_grad_norm_workspace_bytes(len(self.grads)), self.grads[0].device)
+
+
+def mote_clip_grad_norm(clip: GradClip, max_norm: float, norm: torch.Tensor = None) -> torch.Tensor:
+    """Scales the gradients of `clip` to a global norm of at most max_norm; returns that norm before the scaling (fp32 [1]).
+    Calls on one GradClip share its workspace: they must be ordered on one stream."""
+    lib = load_library()
+    dev = clip.grads[0].device
+    with _on_device(grad=clip.grads[0], norm=norm):
+        norm = torch.empty(1, dtype=torch.float32, device=dev) if norm is None else _shape(_dev(norm, torch.float32, "norm"), (1,), "norm")
+        _check(lib.mote_clip_grad_norm(clip.descriptors, len(clip.grads), max_norm, _ptr(norm), _ptr(clip.workspace),
+                                       clip.workspace.numel(), _stream()), "mote_clip_grad_norm")
+    return norm
 
 
 class ForwardGraph:

@@ -203,4 +203,75 @@ hipError_t launch_ste_backward(const uint16_t* dy, const int32_t* offsets_host, 
                                float* dx, float* dw, void* workspace, hipStream_t stream);
 hipError_t launch_copy(void* dst, const void* src, size_t n_bytes, hipStream_t stream);
 
+// Scored routing (mote_route) and its gradient.
+struct RouteArgs {
+  const uint16_t* x;
+  const uint16_t* w_router;
+  const float* bias;        // selection bias or null
+  const uint8_t* mask;      // or null
+  int T, d, E, k;
+  int sigmoid, n_groups, top_groups, group_top, renormalise;
+  float scale;
+  int32_t* topk_idx;
+  float* topk_w;
+  float* logits;            // or null
+  double* part_sum;         // per workgroup: score sums [64] and counts [64], or null
+  int32_t* part_cnt;
+};
+size_t route_workspace_bytes(int T);
+hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, hipStream_t stream);
+struct RouteBackwardArgs {
+  const uint16_t* x;
+  const uint16_t* w_router;
+  const float* logits;
+  const int32_t* topk_idx;
+  const float* d_topk_w;
+  const float* d_score_sum;   // or null
+  const uint8_t* mask;        // or null
+  int T, d, E, k;
+  int sigmoid, renormalise;
+  float scale;
+  float* dx;                  // or null
+  float* dw;                  // or null
+  float* g;                   // [T, 64] dL/dlogits
+};
+size_t route_backward_workspace_bytes(int T, int d, int E);
+hipError_t launch_route_backward(RouteBackwardArgs a, void* workspace, hipStream_t stream);
+// A caller's routing as the dispatch plan wants it: indices outside 0 .. E - 1 become expert 0 with weight 0.
+hipError_t launch_route_import(const int32_t* idx, const float* w, int n, int E, int32_t* topk_idx, float* topk_p, hipStream_t stream);
+
+// Residual sum with the norms on both sides of it, and its gradient; kinds are those of launch_norm_rows, 0: none.
+struct ResidualArgs {
+  int post_kind, pre_kind;
+  float post_eps, pre_eps, residual_scale, branch_scale;
+  const uint16_t* post_gamma;
+  const uint16_t* post_beta;
+  const uint16_t* gate;
+  const uint16_t* pre_gamma;
+  const uint16_t* pre_beta;
+  int T, d;
+};
+struct ResidualGrads {
+  float* gate;
+  float* post_gamma;
+  float* post_beta;
+  float* pre_gamma;
+  float* pre_beta;
+};
+constexpr int kResidualMaxWidth = 8192;
+hipError_t launch_residual_norm(const ResidualArgs& a, bool f32, const void* r, const void* y, void* total, void* normed, hipStream_t stream);
+size_t residual_norm_workspace_bytes(int T, int d);
+hipError_t launch_residual_norm_backward(const ResidualArgs& a, bool f32, const void* r, const void* y, const void* d_total, const void* d_normed, void* dr,
+                                         void* dy, const ResidualGrads& grads, void* workspace, hipStream_t stream);
+
+// Global gradient norm and clipping.
+struct GradTensor {
+  const void* grad;
+  void* out;
+  int64_t n;
+  bool bf16;
+};
+size_t grad_clip_workspace_bytes(int n);
+hipError_t launch_grad_clip(const GradTensor* g, int n, float max_norm, float* norm, void* workspace, hipStream_t stream);
+
 }  // namespace mote

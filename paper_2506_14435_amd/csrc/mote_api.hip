@@ -241,7 +241,7 @@ const char* mote_status_string(int status) {
   }
 }
 
-int mote_version(void) { return 100; }
+int mote_version(void) { return 200; }
 
 size_t mote_packed_bytes(int64_t n_out, int64_t n_in) {
   if (n_out <= 0 || n_in <= 0) return 0;
@@ -354,8 +354,9 @@ namespace {
 
 // The forward pass behind both entry points.  one_stream: everything on the caller's stream and
 // no host-side object is created (no helper stream, no events).
-mote_status forward_impl(const mote_layer* layer, const mote_norm* norm, const void* x, int T, void* out,
-                         void* workspace, size_t workspace_bytes, const mote_taps* taps, void* hip_stream,
+// route_idx, route_w: the caller's routing [T, k] in the place of the layer's router, or null.
+mote_status forward_impl(const mote_layer* layer, const mote_norm* norm, const int32_t* route_idx, const float* route_w, const void* x, int T,
+                         void* out, void* workspace, size_t workspace_bytes, const mote_taps* taps, void* hip_stream,
                          bool one_stream) {
   if (!layer || T < 0) return MOTE_ERR_INVALID_ARG;
   if (norm && (norm->kind != MOTE_NORM_RMS && norm->kind != MOTE_NORM_LAYER)) return MOTE_ERR_INVALID_ARG;
@@ -363,7 +364,7 @@ mote_status forward_impl(const mote_layer* layer, const mote_norm* norm, const v
   if (!batch_ok(layer, T)) return MOTE_ERR_UNSUPPORTED_SHAPE;
   if (T == 0) return MOTE_OK;
   if (!x || !out || !workspace) return MOTE_ERR_INVALID_ARG;
-  if (!layer->w_router || !layer->ws_gate || !layer->ws_up || !layer->ws_down || !layer->wt_gate || !layer->wt_up ||
+  if ((!layer->w_router && !route_idx) || !layer->ws_gate || !layer->ws_up || !layer->ws_down || !layer->wt_gate || !layer->wt_up ||
       !layer->wt_down || !layer->alpha)
     return MOTE_ERR_INVALID_ARG;
   if (layer->shared_bits != 0 && (!layer->ss_gate || !layer->ss_up || !layer->ss_down)) return MOTE_ERR_INVALID_ARG;
@@ -447,8 +448,9 @@ mote_status forward_impl(const mote_layer* layer, const mote_norm* norm, const v
   } else if (fork && shared_weights >= (int64_t{1} << 24)) {
     roles_pay = T <= 32 || (bits == 8 && shared_weights < (int64_t{3} << 23));
   }
-  const bool roles = roles_fit && (roles_pay || roles_knob == 2);
-  const bool local_plan = roles_fit && (roles || plan_pays) && tile_m == 32;
+  // a given routing leaves no router to put beside the shared expert: one kernel takes the routing over, one makes Q_a(x)
+  const bool roles = roles_fit && !route_idx && (roles_pay || roles_knob == 2);
+  const bool local_plan = roles_fit && (roles || plan_pays || route_idx) && tile_m == 32;
   SideStream* side = nullptr;
   if (fork && !roles) MOTE_HIP(side_stream(&side));
   hipStream_t sstream = side ? side->stream : stream;
@@ -512,7 +514,10 @@ mote_status forward_impl(const mote_layer* layer, const mote_norm* norm, const v
   if (roles)
     MOTE_HIP(launch_decode_head(ds, layer->router_bias, static_cast<const uint16_t*>(layer->w_router), E, k, w.topk_idx, w.topk_p,
                                 w.q_x, w.beta_x, w.rs_x, w.h_s, stream));
-  else
+  else if (route_idx) {
+    MOTE_HIP(launch_route_import(route_idx, route_w, R, E, w.topk_idx, w.topk_p, stream));
+    MOTE_HIP(launch_quant_rows(xb, T, d, w.q_x, w.beta_x, w.rs_x, stream));
+  } else
     MOTE_HIP(launch_router_quant(xb, static_cast<const uint16_t*>(layer->w_router), layer->router_bias, T, d, E, k,
                                  w.topk_idx, w.topk_p, w.q_x, w.beta_x, w.rs_x, nullptr, stream));
   MOTE_HIP(mark(1));
@@ -601,6 +606,64 @@ mote_status forward_impl(const mote_layer* layer, const mote_norm* norm, const v
   return MOTE_OK;
 }
 
+// ---- argument checks of the routing, residual and clipping entry points ----
+mote_status routing_bad(const mote_routing* cfg, int T, int d, int E) {
+  if (!cfg || T < 0) return MOTE_ERR_INVALID_ARG;
+  if (cfg->score != MOTE_SCORE_SOFTMAX && cfg->score != MOTE_SCORE_SIGMOID) return MOTE_ERR_INVALID_ARG;
+  if (!std::isfinite(cfg->scale)) return MOTE_ERR_INVALID_ARG;
+  if (d <= 0 || d % 128 || E < 1 || E > 64 || cfg->top_k < 1 || cfg->top_k > E || cfg->top_k > 8) return MOTE_ERR_UNSUPPORTED_SHAPE;
+  if (static_cast<int64_t>(T) * cfg->top_k >= (1 << 24)) return MOTE_ERR_UNSUPPORTED_SHAPE;
+  return MOTE_OK;
+}
+
+mote_status residual_args(const mote_residual* b, int dtype, int T, int d, ResidualArgs* a) {
+  if (!b || T < 0 || (dtype != MOTE_DTYPE_F32 && dtype != MOTE_DTYPE_BF16)) return MOTE_ERR_INVALID_ARG;
+  if (!std::isfinite(b->residual_scale) || !std::isfinite(b->branch_scale)) return MOTE_ERR_INVALID_ARG;
+  for (const mote_norm* n : {b->post, b->pre}) {
+    if (!n) continue;
+    if ((n->kind != MOTE_NORM_RMS && n->kind != MOTE_NORM_LAYER) || !n->gamma || (n->kind == MOTE_NORM_LAYER && !n->beta)) return MOTE_ERR_INVALID_ARG;
+    if (!(n->eps >= 0.0) || !std::isfinite(n->eps)) return MOTE_ERR_INVALID_ARG;
+  }
+  if (d < 8 || d % 8 || d > kResidualMaxWidth) return MOTE_ERR_UNSUPPORTED_SHAPE;
+  *a = ResidualArgs{};
+  if (b->post) {
+    a->post_kind = b->post->kind;
+    a->post_eps = static_cast<float>(b->post->eps);
+    a->post_gamma = static_cast<const uint16_t*>(b->post->gamma);
+    if (a->post_kind == MOTE_NORM_LAYER) a->post_beta = static_cast<const uint16_t*>(b->post->beta);
+  }
+  if (b->pre) {
+    a->pre_kind = b->pre->kind;
+    a->pre_eps = static_cast<float>(b->pre->eps);
+    a->pre_gamma = static_cast<const uint16_t*>(b->pre->gamma);
+    if (a->pre_kind == MOTE_NORM_LAYER) a->pre_beta = static_cast<const uint16_t*>(b->pre->beta);
+  }
+  a->gate = static_cast<const uint16_t*>(b->gate);
+  a->residual_scale = b->residual_scale;
+  a->branch_scale = b->branch_scale;
+  a->T = T;
+  a->d = d;
+  return MOTE_OK;
+}
+
+constexpr int kMaxGradTensors = 4096;
+struct ByteRange {
+  uintptr_t from, to;
+  bool written;
+};
+// Whether a written range meets any other range.  In order of their starts, a range can meet an earlier one only if the
+// farthest end of the earlier ones (of the written ones, for a range that is only read) lies behind its start.
+bool written_ranges_overlap(ByteRange* r, int n) {
+  std::sort(r, r + n, [](const ByteRange& a, const ByteRange& b) { return a.from < b.from; });
+  uintptr_t end = 0, end_written = 0;
+  for (int i = 0; i < n; ++i) {
+    if (r[i].from < (r[i].written ? end : end_written)) return true;
+    end = std::max(end, r[i].to);
+    if (r[i].written) end_written = std::max(end_written, r[i].to);
+  }
+  return false;
+}
+
 // ---- scratch of mote_layer_forward_static: one array per device, held until the process ends ----
 __device__ __align__(256) unsigned char scratch[MOTE_STATIC_WORKSPACE_BYTES];
 void* g_scratch_ptr[16] = {};   // device address of `scratch` on each device (the array's name is
@@ -627,13 +690,20 @@ extern "C" {
 
 mote_status mote_layer_forward(const mote_layer* layer, const void* x, int T, void* out, void* workspace,
                                size_t workspace_bytes, const mote_taps* taps, void* hip_stream) {
-  return forward_impl(layer, nullptr, x, T, out, workspace, workspace_bytes, taps, hip_stream, false);
+  return forward_impl(layer, nullptr, nullptr, nullptr, x, T, out, workspace, workspace_bytes, taps, hip_stream, false);
+}
+
+mote_status mote_layer_forward_routed(const mote_layer* layer, const void* x, int T, const int32_t* topk_idx,
+                                      const float* topk_w, void* out, void* workspace, size_t workspace_bytes,
+                                      const mote_taps* taps, void* hip_stream) {
+  if (T > 0 && (!topk_idx || !topk_w)) return MOTE_ERR_INVALID_ARG;
+  return forward_impl(layer, nullptr, topk_idx, topk_w, x, T, out, workspace, workspace_bytes, taps, hip_stream, false);
 }
 
 mote_status mote_block_forward(const mote_layer* layer, const mote_norm* norm, const void* x_a, int T, void* out,
                                void* workspace, size_t workspace_bytes, const mote_taps* taps, void* hip_stream) {
   if (!norm) return MOTE_ERR_INVALID_ARG;
-  return forward_impl(layer, norm, x_a, T, out, workspace, workspace_bytes, taps, hip_stream, false);
+  return forward_impl(layer, norm, nullptr, nullptr, x_a, T, out, workspace, workspace_bytes, taps, hip_stream, false);
 }
 
 mote_status mote_layer_forward_static(const mote_layer* layer, const void* x, int T, void* out,
@@ -648,7 +718,7 @@ mote_status mote_layer_forward_static(const mote_layer* layer, const void* x, in
   // Nothing in the array has to start at zero: the dispatch plan kernel zeroes the tile counters and the plane words for
   // the large-batch kernels (a step that makes its plan inside the gate-up kernel uses neither), everything else is
   // written before it is read.
-  return forward_impl(layer, nullptr, x, T, out, ws, MOTE_STATIC_WORKSPACE_BYTES, taps, hip_stream, true);
+  return forward_impl(layer, nullptr, nullptr, nullptr, x, T, out, ws, MOTE_STATIC_WORKSPACE_BYTES, taps, hip_stream, true);
 }
 
 mote_status mote_stage_timing(int enable) {
@@ -711,6 +781,130 @@ mote_status mote_ste_linear_backward(const void* dy, const int32_t* offsets_host
   if (ste_backward_workspace_bytes(R, N, K, E) > workspace_bytes) return MOTE_ERR_WORKSPACE_TOO_SMALL;
   MOTE_HIP(launch_ste_backward(static_cast<const uint16_t*>(dy), offsets_host, packed, alpha, alpha_stride, q, beta, R, N,
                                K, E, dx, dw, workspace, static_cast<hipStream_t>(hip_stream)));
+  return MOTE_OK;
+}
+
+size_t mote_route_workspace_bytes(int T, int E) {
+  if (T < 0 || E < 1 || E > 64) return 0;
+  return route_workspace_bytes(T);
+}
+
+mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_router, const float* select_bias,
+                       const uint8_t* token_mask, int T, int d, int E, int32_t* topk_idx, float* topk_w, float* logits,
+                       int32_t* expert_counts, float* score_sum, void* workspace, size_t workspace_bytes,
+                       void* hip_stream) {
+  const mote_status bad = routing_bad(cfg, T, d, E);
+  if (bad != MOTE_OK) return bad;
+  const int k = cfg->top_k, G = cfg->n_groups;
+  if (G < 1 || G > E || E % G || cfg->top_groups < 1 || cfg->top_groups > G || cfg->group_top < 1 || cfg->group_top > 2) return MOTE_ERR_INVALID_ARG;
+  if (G > 1 && (cfg->group_top > E / G || k > cfg->top_groups * (E / G))) return MOTE_ERR_UNSUPPORTED_SHAPE;
+  if (T > 0 && (!x || !w_router || !topk_idx || !topk_w)) return MOTE_ERR_INVALID_ARG;
+  if (expert_counts || score_sum) {
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOTE_ERR_INVALID_ARG;
+    if (workspace_bytes < route_workspace_bytes(T)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
+  }
+  if (T == 0 && !expert_counts && !score_sum) return MOTE_OK;
+  RouteArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_router), select_bias, token_mask, T, d, E, k,
+              cfg->score == MOTE_SCORE_SIGMOID, G, cfg->top_groups, cfg->group_top, cfg->renormalise != 0, cfg->scale,
+              topk_idx, topk_w, logits, nullptr, nullptr};
+  MOTE_HIP(launch_route(a, expert_counts, score_sum, workspace, static_cast<hipStream_t>(hip_stream)));
+  return MOTE_OK;
+}
+
+size_t mote_route_backward_workspace_bytes(int T, int d, int E) {
+  if (T < 0 || d <= 0 || d % 128 || E < 1 || E > 64) return 0;
+  return route_backward_workspace_bytes(T, d, E);
+}
+
+mote_status mote_route_backward(const mote_routing* cfg, const void* x, const void* w_router, const float* logits,
+                                const int32_t* topk_idx, const float* d_topk_w, const float* d_score_sum,
+                                const uint8_t* token_mask, int T, int d, int E, float* dx, float* dw_router,
+                                void* workspace, size_t workspace_bytes, void* hip_stream) {
+  const mote_status bad = routing_bad(cfg, T, d, E);
+  if (bad != MOTE_OK) return bad;
+  if (!dx && !dw_router) return MOTE_OK;
+  if (T > 0 && (!x || !w_router || !logits || !topk_idx || !d_topk_w)) return MOTE_ERR_INVALID_ARG;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOTE_ERR_INVALID_ARG;
+  if (workspace_bytes < route_backward_workspace_bytes(T, d, E)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
+  RouteBackwardArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_router), logits, topk_idx, d_topk_w, d_score_sum, token_mask,
+                      T, d, E, cfg->top_k, cfg->score == MOTE_SCORE_SIGMOID, cfg->renormalise != 0, cfg->scale, dx, dw_router, nullptr};
+  MOTE_HIP(launch_route_backward(a, workspace, static_cast<hipStream_t>(hip_stream)));
+  return MOTE_OK;
+}
+
+mote_status mote_residual_norm(const mote_residual* block, const void* r, const void* y, int dtype, int T, int d,
+                               void* total, void* normed, void* hip_stream) {
+  ResidualArgs a;
+  const mote_status bad = residual_args(block, dtype, T, d, &a);
+  if (bad != MOTE_OK || T == 0) return bad;
+  if (!r || !y || !total || (block->pre && !normed)) return MOTE_ERR_INVALID_ARG;
+  MOTE_HIP(launch_residual_norm(a, dtype == MOTE_DTYPE_F32, r, y, total, normed, static_cast<hipStream_t>(hip_stream)));
+  return MOTE_OK;
+}
+
+size_t mote_residual_norm_workspace_bytes(const mote_residual* block, int T, int d) {
+  ResidualArgs a;
+  if (residual_args(block, MOTE_DTYPE_BF16, T, d, &a) != MOTE_OK) return 0;
+  return residual_norm_workspace_bytes(T, d);
+}
+
+mote_status mote_residual_norm_backward(const mote_residual* block, const void* r, const void* y, const void* d_total,
+                                        const void* d_normed, int dtype, int T, int d, void* dr, void* dy,
+                                        const mote_residual_grads* grads, void* workspace, size_t workspace_bytes,
+                                        void* hip_stream) {
+  ResidualArgs a;
+  const mote_status bad = residual_args(block, dtype, T, d, &a);
+  if (bad != MOTE_OK) return bad;
+  if (T > 0 && (!r || !y || !dr || !dy)) return MOTE_ERR_INVALID_ARG;
+  if (d_normed && !block->pre) return MOTE_ERR_INVALID_ARG;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOTE_ERR_INVALID_ARG;
+  if (workspace_bytes < residual_norm_workspace_bytes(T, d)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
+  ResidualGrads g{};
+  if (grads) {
+    if (block->gate) g.gate = grads->gate;
+    if (block->post) g.post_gamma = grads->post_gamma;
+    if (block->post && a.post_kind == MOTE_NORM_LAYER) g.post_beta = grads->post_beta;
+    if (block->pre) g.pre_gamma = grads->pre_gamma;
+    if (block->pre && a.pre_kind == MOTE_NORM_LAYER) g.pre_beta = grads->pre_beta;
+  }
+  MOTE_HIP(launch_residual_norm_backward(a, dtype == MOTE_DTYPE_F32, r, y, d_total, d_normed, dr, dy, g, workspace,
+                                         static_cast<hipStream_t>(hip_stream)));
+  return MOTE_OK;
+}
+
+size_t mote_clip_grad_norm_workspace_bytes(int n_tensors) {
+  if (n_tensors < 0 || n_tensors > kMaxGradTensors) return 0;
+  return grad_clip_workspace_bytes(n_tensors);
+}
+
+mote_status mote_clip_grad_norm(const mote_grad* grads_host, int n_tensors, float max_norm, float* norm, void* workspace,
+                                size_t workspace_bytes, void* hip_stream) {
+  if (n_tensors < 0 || (n_tensors > 0 && !grads_host) || !norm || !(max_norm > 0.0f)) return MOTE_ERR_INVALID_ARG;
+  if (n_tensors > kMaxGradTensors) return MOTE_ERR_UNSUPPORTED_SHAPE;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOTE_ERR_INVALID_ARG;
+  GradTensor g[kMaxGradTensors];
+  ByteRange span[2 * kMaxGradTensors];   // what is written, and the gradients that are only read
+  int n_span = 0;
+  int64_t total = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const mote_grad& s = grads_host[i];
+    if (s.dtype != MOTE_DTYPE_F32 && s.dtype != MOTE_DTYPE_BF16) return MOTE_ERR_INVALID_ARG;
+    if (s.n < 0) return MOTE_ERR_INVALID_ARG;
+    if (s.n >= (int64_t{1} << 40)) return MOTE_ERR_UNSUPPORTED_SHAPE;
+    const uintptr_t size = s.dtype == MOTE_DTYPE_BF16 ? 2 : 4;
+    void* const out = s.out ? s.out : const_cast<void*>(s.grad);
+    g[i] = GradTensor{s.grad, out, s.n, size == 2};
+    if (s.n == 0) continue;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(s.grad), to = reinterpret_cast<uintptr_t>(out);
+    if (!from || from % size || to % size) return MOTE_ERR_INVALID_ARG;
+    total += s.n;
+    span[n_span++] = ByteRange{to, to + static_cast<uintptr_t>(s.n) * size, true};
+    if (from != to) span[n_span++] = ByteRange{from, from + static_cast<uintptr_t>(s.n) * size, false};
+  }
+  if (total >= (int64_t{1} << 44)) return MOTE_ERR_UNSUPPORTED_SHAPE;
+  if (written_ranges_overlap(span, n_span)) return MOTE_ERR_INVALID_ARG;
+  if (workspace_bytes < grad_clip_workspace_bytes(n_tensors)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
+  MOTE_HIP(launch_grad_clip(g, n_tensors, max_norm, norm, workspace, static_cast<hipStream_t>(hip_stream)));
   return MOTE_OK;
 }
 

@@ -1,0 +1,351 @@
+// The residual stream between two branches of a block: total = a r + b gate * N_post(y), normed = N_pre(total), and its
+// gradient.  N is RMSNorm or layer normalisation as in block_extras.hip, here in fp32 throughout.
+//
+// A row is held in registers between its loads and its stores: NT threads, 8 channels each (NT * 8 >= d), every row
+// quantity (mean, variance, the two means of a norm's gradient) is a sum over those threads.  A workgroup keeps the
+// parameters of its channels in registers and walks over rows.  Bound: HBM, 8 bytes per bf16 element forward, 12 backward.
+#include <algorithm>
+
+#include "common.h"
+#include "launch.h"
+
+namespace mote {
+
+namespace {
+
+// 8 values of a row: raw as loaded, and as fp32
+template <typename T> struct Row8;
+template <> struct Row8<uint16_t> {
+  uint4 p;
+  __device__ __forceinline__ void load(const uint16_t* s) { p = *reinterpret_cast<const uint4*>(s); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = bf16_lo(p.x); v[1] = bf16_hi(p.x); v[2] = bf16_lo(p.y); v[3] = bf16_hi(p.y);
+    v[4] = bf16_lo(p.z); v[5] = bf16_hi(p.z); v[6] = bf16_lo(p.w); v[7] = bf16_hi(p.w);
+  }
+  static __device__ __forceinline__ void store(uint16_t* d, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(d) = make_uint4(cvt_pk_bf16(v[0], v[1]), cvt_pk_bf16(v[2], v[3]), cvt_pk_bf16(v[4], v[5]), cvt_pk_bf16(v[6], v[7]));
+  }
+};
+template <> struct Row8<float> {
+  float4 p, q;
+  __device__ __forceinline__ void load(const float* s) { p = reinterpret_cast<const float4*>(s)[0]; q = reinterpret_cast<const float4*>(s)[1]; }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = p.x; v[1] = p.y; v[2] = p.z; v[3] = p.w; v[4] = q.x; v[5] = q.y; v[6] = q.z; v[7] = q.w;
+  }
+  static __device__ __forceinline__ void store(float* d, const float (&v)[8]) {
+    reinterpret_cast<float4*>(d)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(d)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+};
+
+// Parameters of a thread's 8 channels (absent ones: the neutral value)
+__device__ __forceinline__ void load_param(const uint16_t* p, bool in, int c, float neutral, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = neutral;
+  if (p != nullptr && in) {
+    Row8<uint16_t> r;
+    r.load(p + c);
+    r.get(v);
+  }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+// Sum over the wavefront, the same in every lane: four steps inside rows of 16 lanes, then the four rows
+__device__ __forceinline__ float wave_sum_f(float v) {
+  v = dpp_add<0xB1>(v);    // lane ^ 1
+  v = dpp_add<0x4E>(v);    // lane ^ 2
+  v = dpp_add<0x141>(v);   // half-row mirror
+  v = dpp_add<0x140>(v);   // row mirror
+  const int b = __float_as_int(v);
+  return (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
+         (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
+}
+
+// Sums over the NT threads of a row; buf alternates so that one barrier per sum is enough.
+template <int NT>
+struct RowSum {
+  static constexpr int kWaves = NT / 64;
+  float (*buf)[2];   // LDS: [2 * kWaves] of this row
+  int turn = 0;
+  __device__ __forceinline__ void operator()(float& a, float& b) {
+    a = wave_sum_f(a);
+    b = wave_sum_f(b);
+    if constexpr (NT > 64) {
+      float (*const s)[2] = buf + (turn ? kWaves : 0);
+      turn ^= 1;
+      const int w = (threadIdx.x % NT) >> 6;
+      if ((threadIdx.x & 63) == 0) { s[w][0] = a; s[w][1] = b; }
+      __syncthreads();
+      a = 0.0f;
+      b = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) { a += s[i][0]; b += s[i][1]; }
+    }
+  }
+  __device__ __forceinline__ float operator()(float a) {
+    float b = 0.0f;
+    (*this)(a, b);
+    return a;
+  }
+};
+
+template <int NT> constexpr int rows_of_block() { return NT < 256 ? 256 / NT : 1; }
+template <int NT> constexpr int block_threads() { return NT < 256 ? 256 : NT; }
+
+// Normalises v in place to its hat (no gamma, beta); returns 1 / sqrt(var + eps).  Channels beyond d hold zero and stay zero.
+template <int NT>
+__device__ __forceinline__ float normalise(RowSum<NT>& sum, int kind, float eps, float inv_d, bool in, float (&v)[8]) {
+  if (kind == 2) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += v[i];
+    const float mean = sum(s) * inv_d;
+    if (in)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] -= mean;
+  }
+  float q = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q = fmaf(v[i], v[i], q);
+  const float inv = 1.0f / sqrtf(sum(q) * inv_d + eps);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] *= inv;
+  return inv;
+}
+
+template <int NT, typename T>
+__global__ __launch_bounds__(block_threads<NT>()) void residual_norm_kernel(ResidualArgs a, const T* __restrict__ r, const T* __restrict__ y,
+                                                                            T* __restrict__ total, T* __restrict__ normed) {
+  constexpr int kRows = rows_of_block<NT>();
+  __shared__ float s_buf[kRows][2 * (NT / 64)][2];
+  const int slot = threadIdx.x / NT, c = (threadIdx.x % NT) * 8;
+  const bool in = c < a.d;
+  RowSum<NT> sum{s_buf[slot]};
+  float g_post[8], b_post[8], gate[8], g_pre[8], b_pre[8];
+  load_param(a.post_gamma, in, c, 1.0f, g_post);
+  load_param(a.post_beta, in, c, 0.0f, b_post);
+  load_param(a.gate, in, c, 1.0f, gate);
+  load_param(a.pre_gamma, in, c, 1.0f, g_pre);
+  load_param(a.pre_beta, in, c, 0.0f, b_pre);
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.T; row0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    const bool live = row0 + slot < a.T;
+    const int64_t at = min(row0 + slot, static_cast<int64_t>(a.T) - 1) * a.d + c;
+    float rv[8] = {}, v[8] = {};
+    if (in) {
+      Row8<T> rr, yy;
+      yy.load(y + at);
+      rr.load(r + at);
+      yy.get(v);
+      rr.get(rv);
+    }
+    if (a.post_kind) {
+      normalise(sum, a.post_kind, a.post_eps, inv_d, in, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], g_post[i], b_post[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(a.residual_scale, rv[i], a.branch_scale * (gate[i] * v[i]));
+    if (in && live) Row8<T>::store(total + at, v);
+    if (a.pre_kind) {
+      normalise(sum, a.pre_kind, a.pre_eps, inv_d, in, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = fmaf(v[i], g_pre[i], b_pre[i]);
+      if (in && live) Row8<T>::store(normed + at, v);
+    }
+  }
+}
+
+// Gradient.  The workgroup's sums for the parameters of a thread's channels stay in registers over its rows and leave as one
+// partial row per row slot: partial[(block * kRows + slot)][5][d], summed by residual_params_kernel.
+template <int NT, typename T>
+__global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_kernel(ResidualArgs a, const T* __restrict__ r, const T* __restrict__ y,
+                                                                                     const T* __restrict__ d_total, const T* __restrict__ d_normed,
+                                                                                     T* __restrict__ dr, T* __restrict__ dy, float* __restrict__ partial) {
+  constexpr int kRows = rows_of_block<NT>();
+  __shared__ float s_buf[kRows][2 * (NT / 64)][2];
+  const int slot = threadIdx.x / NT, c = (threadIdx.x % NT) * 8;
+  const bool in = c < a.d;
+  RowSum<NT> sum{s_buf[slot]};
+  float g_post[8], b_post[8], gate[8], g_pre[8];
+  load_param(a.post_gamma, in, c, 1.0f, g_post);
+  load_param(a.post_beta, in, c, 0.0f, b_post);
+  load_param(a.gate, in, c, 1.0f, gate);
+  load_param(a.pre_gamma, in, c, 1.0f, g_pre);
+  float p_gate[8] = {}, p_post_g[8] = {}, p_post_b[8] = {}, p_pre_g[8] = {}, p_pre_b[8] = {};
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.T; row0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    const bool live = row0 + slot < a.T;
+    const int64_t at = min(row0 + slot, static_cast<int64_t>(a.T) - 1) * a.d + c;
+    float rv[8] = {}, hat_y[8] = {}, up[8] = {}, dn[8] = {};
+    if (in) {
+      Row8<T> q;
+      q.load(y + at);
+      q.get(hat_y);
+      q.load(r + at);
+      q.get(rv);
+      if (d_normed != nullptr) { q.load(d_normed + at); q.get(dn); }
+      if (d_total != nullptr) { q.load(d_total + at); q.get(up); }
+    }
+    float z[8], inv_y = 1.0f;
+    if (a.post_kind) {
+      inv_y = normalise(sum, a.post_kind, a.post_eps, inv_d, in, hat_y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = fmaf(hat_y[i], g_post[i], b_post[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) z[i] = hat_y[i];
+    }
+    if (d_normed != nullptr) {
+      float hat[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) hat[i] = fmaf(a.residual_scale, rv[i], a.branch_scale * (gate[i] * z[i]));
+      const float inv = normalise(sum, a.pre_kind, a.pre_eps, inv_d, in, hat);
+      float m1 = 0.0f, m2 = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (live) {
+          p_pre_g[i] = fmaf(dn[i], hat[i], p_pre_g[i]);
+          p_pre_b[i] += dn[i];
+        }
+        dn[i] *= g_pre[i];
+        m1 += dn[i];
+        m2 = fmaf(dn[i], hat[i], m2);
+      }
+      sum(m1, m2);
+      m1 = a.pre_kind == 2 ? m1 * inv_d : 0.0f;
+      m2 *= inv_d;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) up[i] = fmaf(inv, dn[i] - m1 - hat[i] * m2, up[i]);
+    }
+    if (in && live) {
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = a.residual_scale * up[i];
+      Row8<T>::store(dr + at, o);
+    }
+    float dz[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float bu = in ? a.branch_scale * up[i] : 0.0f;
+      if (live) p_gate[i] = fmaf(bu, z[i], p_gate[i]);
+      dz[i] = bu * gate[i];
+    }
+    if (a.post_kind) {
+      float m1 = 0.0f, m2 = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (live) {
+          p_post_g[i] = fmaf(dz[i], hat_y[i], p_post_g[i]);
+          p_post_b[i] += dz[i];
+        }
+        dz[i] *= g_post[i];
+        m1 += dz[i];
+        m2 = fmaf(dz[i], hat_y[i], m2);
+      }
+      sum(m1, m2);
+      m1 = a.post_kind == 2 ? m1 * inv_d : 0.0f;
+      m2 *= inv_d;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dz[i] = inv_y * (dz[i] - m1 - hat_y[i] * m2);
+    }
+    if (in && live) Row8<T>::store(dy + at, dz);
+  }
+  if (partial != nullptr && in) {
+    float* const p = partial + (static_cast<int64_t>(blockIdx.x) * kRows + slot) * 5 * a.d + c;
+    Row8<float>::store(p, p_gate);
+    Row8<float>::store(p + a.d, p_post_g);
+    Row8<float>::store(p + 2 * a.d, p_post_b);
+    Row8<float>::store(p + 3 * a.d, p_pre_g);
+    Row8<float>::store(p + 4 * a.d, p_pre_b);
+  }
+}
+
+// Sums of the partial rows in their order: 64 columns per workgroup, 16 slices of the rows.
+__global__ __launch_bounds__(1024) void residual_params_kernel(const float* __restrict__ partial, int rows, int d, ResidualGrads out) {
+  __shared__ float s_p[16][64];
+  const int which = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6;
+  float* const dst = which == 0 ? out.gate : which == 1 ? out.post_gamma : which == 2 ? out.post_beta : which == 3 ? out.pre_gamma : out.pre_beta;
+  if (dst == nullptr) return;
+  float s = 0.0f;
+  if (c < d)
+    for (int i = part; i < rows; i += 16) s += partial[(static_cast<int64_t>(i) * 5 + which) * d + c];
+  s_p[part][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (part == 0 && c < d) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += s_p[i][threadIdx.x];
+    dst[c] = s;
+  }
+}
+
+template <int NT, typename T>
+void forward(const ResidualArgs& a, const void* r, const void* y, void* total, void* normed, hipStream_t stream) {
+  constexpr int kRows = rows_of_block<NT>();
+  const int blocks = static_cast<int>(std::min<int64_t>((static_cast<int64_t>(a.T) + kRows - 1) / kRows, 2048));
+  residual_norm_kernel<NT, T><<<blocks, block_threads<NT>(), 0, stream>>>(a, static_cast<const T*>(r), static_cast<const T*>(y), static_cast<T*>(total),
+                                                                          static_cast<T*>(normed));
+}
+
+int threads_of_row(int d) {
+  int nt = 64;
+  while (nt * 8 < d) nt *= 2;
+  return nt;
+}
+int backward_blocks(int T, int d) {
+  const int rows = std::max(256 / threads_of_row(d), 1);
+  return std::min((T + rows - 1) / rows, 512);
+}
+
+template <int NT, typename T>
+void backward(const ResidualArgs& a, const void* r, const void* y, const void* d_total, const void* d_normed, void* dr, void* dy, float* partial,
+              hipStream_t stream) {
+  residual_norm_backward_kernel<NT, T><<<backward_blocks(a.T, a.d), block_threads<NT>(), 0, stream>>>(
+      a, static_cast<const T*>(r), static_cast<const T*>(y), static_cast<const T*>(d_total), static_cast<const T*>(d_normed), static_cast<T*>(dr),
+      static_cast<T*>(dy), partial);
+}
+
+}  // namespace
+
+#define MOTE_ROW_DISPATCH(CALL)                 \
+  switch (threads_of_row(a.d)) {                \
+    case 64: CALL(64); break;                   \
+    case 128: CALL(128); break;                 \
+    case 256: CALL(256); break;                 \
+    case 512: CALL(512); break;                 \
+    default: CALL(1024); break;                 \
+  }
+
+hipError_t launch_residual_norm(const ResidualArgs& a, bool f32, const void* r, const void* y, void* total, void* normed, hipStream_t stream) {
+#define MOTE_CALL(NT) f32 ? forward<NT, float>(a, r, y, total, normed, stream) : forward<NT, uint16_t>(a, r, y, total, normed, stream)
+  MOTE_ROW_DISPATCH(MOTE_CALL)
+#undef MOTE_CALL
+  return hipGetLastError();
+}
+
+size_t residual_norm_workspace_bytes(int T, int d) {
+  const size_t rows = static_cast<size_t>(backward_blocks(std::max(T, 1), d)) * std::max(256 / threads_of_row(d), 1);
+  return 256 + rows * 5 * d * sizeof(float);
+}
+
+hipError_t launch_residual_norm_backward(const ResidualArgs& a, bool f32, const void* r, const void* y, const void* d_total, const void* d_normed, void* dr,
+                                         void* dy, const ResidualGrads& grads, void* workspace, hipStream_t stream) {
+  const bool params = grads.gate || grads.post_gamma || grads.post_beta || grads.pre_gamma || grads.pre_beta;
+  float* const partial = params ? static_cast<float*>(workspace) : nullptr;
+  int rows = 0;
+  if (a.T > 0) {
+    rows = backward_blocks(a.T, a.d) * std::max(256 / threads_of_row(a.d), 1);
+#define MOTE_CALL(NT)                                                                                      \
+  f32 ? backward<NT, float>(a, r, y, d_total, d_normed, dr, dy, partial, stream)                            \
+      : backward<NT, uint16_t>(a, r, y, d_total, d_normed, dr, dy, partial, stream)
+    MOTE_ROW_DISPATCH(MOTE_CALL)
+#undef MOTE_CALL
+  }
+  if (params) residual_params_kernel<<<dim3((a.d + 63) / 64, 5), 1024, 0, stream>>>(partial, rows, a.d, grads);
+  return hipGetLastError();
+}
+
+}  // namespace mote
