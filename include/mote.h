@@ -200,9 +200,9 @@ mote_status mote_router_balance(const void* x, const void* w_router, const float
  * expert_counts out: int32 [E] or NULL; number of (token, slot) pairs of each expert
  * score_sum    out: fp32 [E] or NULL; sum over the tokens of s (fp64 sums in a fixed order): with expert_counts the two
  *                   factors of Eq.12
- * workspace       : device, >= mote_route_workspace_bytes(T, E), 256-byte aligned; may be NULL when expert_counts and
- *                   score_sum are
- * Limits: d % 128 == 0, 1 <= E <= 64, T * top_k < 2^24; T == 0 leaves counts and sums zero.
+ * workspace       : device, >= mote_route_workspace_bytes(T, d, E), 256-byte aligned; up to 64 tokens it may be NULL when
+ *                   expert_counts and score_sum are
+ * Limits: d % 128 == 0, d <= 65536, 1 <= E <= 64, T * top_k < 2^24; T == 0 leaves counts and sums zero.
  * Softmax without groups, bias and renormalise selects as mote_router_topk does (finite logits). */
 enum { MOTE_SCORE_SOFTMAX = 0, MOTE_SCORE_SIGMOID = 1 };
 typedef struct {
@@ -214,7 +214,7 @@ typedef struct {
   int renormalise;  /* 0: weights are scores, else they add up to scale  */
   float scale;      /* finite                                            */
 } mote_routing;
-size_t mote_route_workspace_bytes(int T, int E);
+size_t mote_route_workspace_bytes(int T, int d, int E);
 mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_router, const float* select_bias,
                        const uint8_t* token_mask, int T, int d, int E, int32_t* topk_idx, float* topk_w, float* logits,
                        int32_t* expert_counts, float* score_sum, void* workspace, size_t workspace_bytes,

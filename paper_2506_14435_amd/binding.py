@@ -129,7 +129,7 @@ def load_library() -> ctypes.CDLL:
                                              c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p,
                                              c_size_t, c_void_p]
     lib.mote_route_workspace_bytes.restype = c_size_t
-    lib.mote_route_workspace_bytes.argtypes = [c_int, c_int]
+    lib.mote_route_workspace_bytes.argtypes = [c_int, c_int, c_int]
     lib.mote_route.restype = c_int
     lib.mote_route.argtypes = [POINTER(MoteRoutingStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
                                c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
@@ -553,7 +553,8 @@ def mote_route(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRouting, se
         if want_stats:
             counts = torch.empty(n_exp, dtype=torch.int32, device=dev)
             score_sum = torch.empty(n_exp, dtype=torch.float32, device=dev)
-            workspace = _workspace(workspace, lib.mote_route_workspace_bytes(n_tok, n_exp), dev)
+        if want_stats or n_tok > 64:
+            workspace = _workspace(workspace, lib.mote_route_workspace_bytes(n_tok, d, n_exp), dev)
         _check(lib.mote_route(ctypes.byref(routing.struct), _ptr(x), _ptr(w_router), _ptr(select_bias), _ptr(token_mask), n_tok, d,
                               n_exp, _ptr(idx), _ptr(wt), _ptr(logits), _ptr(counts), _ptr(score_sum), _ptr(workspace),
                               workspace.numel() if workspace is not None else 0, _stream()), "mote_route")

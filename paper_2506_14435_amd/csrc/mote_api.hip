@@ -611,7 +611,7 @@ mote_status routing_bad(const mote_routing* cfg, int T, int d, int E) {
   if (!cfg || T < 0) return MOTE_ERR_INVALID_ARG;
   if (cfg->score != MOTE_SCORE_SOFTMAX && cfg->score != MOTE_SCORE_SIGMOID) return MOTE_ERR_INVALID_ARG;
   if (!std::isfinite(cfg->scale)) return MOTE_ERR_INVALID_ARG;
-  if (d <= 0 || d % 128 || E < 1 || E > 64 || cfg->top_k < 1 || cfg->top_k > E || cfg->top_k > 8) return MOTE_ERR_UNSUPPORTED_SHAPE;
+  if (d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64 || cfg->top_k < 1 || cfg->top_k > E || cfg->top_k > 8) return MOTE_ERR_UNSUPPORTED_SHAPE;
   if (static_cast<int64_t>(T) * cfg->top_k >= (1 << 24)) return MOTE_ERR_UNSUPPORTED_SHAPE;
   return MOTE_OK;
 }
@@ -784,9 +784,9 @@ mote_status mote_ste_linear_backward(const void* dy, const int32_t* offsets_host
   return MOTE_OK;
 }
 
-size_t mote_route_workspace_bytes(int T, int E) {
-  if (T < 0 || E < 1 || E > 64) return 0;
-  return route_workspace_bytes(T);
+size_t mote_route_workspace_bytes(int T, int d, int E) {
+  if (T < 0 || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
+  return route_workspace_bytes(T, d, E, true);
 }
 
 mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_router, const float* select_bias,
@@ -799,20 +799,21 @@ mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_rou
   if (G < 1 || G > E || E % G || cfg->top_groups < 1 || cfg->top_groups > G || cfg->group_top < 1 || cfg->group_top > 2) return MOTE_ERR_INVALID_ARG;
   if (G > 1 && (cfg->group_top > E / G || k > cfg->top_groups * (E / G))) return MOTE_ERR_UNSUPPORTED_SHAPE;
   if (T > 0 && (!x || !w_router || !topk_idx || !topk_w)) return MOTE_ERR_INVALID_ARG;
-  if (expert_counts || score_sum) {
+  const bool stats = expert_counts || score_sum;
+  if (stats || T > kRouteFewTokens) {
     if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOTE_ERR_INVALID_ARG;
-    if (workspace_bytes < route_workspace_bytes(T)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < route_workspace_bytes(T, d, E, stats)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
   }
-  if (T == 0 && !expert_counts && !score_sum) return MOTE_OK;
+  if (T == 0 && !stats) return MOTE_OK;
   RouteArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_router), select_bias, token_mask, T, d, E, k,
               cfg->score == MOTE_SCORE_SIGMOID, G, cfg->top_groups, cfg->group_top, cfg->renormalise != 0, cfg->scale,
-              topk_idx, topk_w, logits, nullptr, nullptr};
+              topk_idx, topk_w, logits, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   MOTE_HIP(launch_route(a, expert_counts, score_sum, workspace, static_cast<hipStream_t>(hip_stream)));
   return MOTE_OK;
 }
 
 size_t mote_route_backward_workspace_bytes(int T, int d, int E) {
-  if (T < 0 || d <= 0 || d % 128 || E < 1 || E > 64) return 0;
+  if (T < 0 || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
   return route_backward_workspace_bytes(T, d, E);
 }
 

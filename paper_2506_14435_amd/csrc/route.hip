@@ -1,6 +1,7 @@
 // Scored routing (softmax or sigmoid scores, selection bias, groups, top-k, renormalised weights) and its gradient.
 #include <algorithm>
 #include <cfloat>
+#include <climits>
 
 #include "common.h"
 #include "launch.h"
@@ -20,10 +21,11 @@ constexpr int kRtWaves = 8;
 constexpr int kRtThreads = 64 * kRtWaves;
 constexpr int kRtUnit = 64;       // channels of a unit
 constexpr int kRtRow = 65;        // elements of an LDS row of 64 logits or keys: the rows of a wavefront's four tokens start in different banks
-// Bound of a unit's rounding, in units of 2^-24 |x| |w| (Euclidean norms, which bound sum |x w|): four chained instructions, each
-// of which aligns 16 products and the addend to the largest of them; measured at most 6.1 units of sum |x w| per instruction
-// over normal, one-signed, wide-range and one-large inputs, taken as 16.  Plus the rounding of a logit to fp32.
-constexpr float kRtBound = (4 * 16 + 2) * 0x1p-24f * 1.02f;
+// How far a logit may be off, in units of 2^-24 |x| |w| (Euclidean norms, which bound sum |x w|): a unit is a chain of four
+// instructions, each of which aligns 16 products and the addend to the largest of them.  Measured at most 6.9 units of the
+// unit's own sum |x w| over normal, one-signed, wide-range and one-large inputs (1.9 for normal ones, and the errors of the
+// units of a row add up like random signs); taken as 8 in every unit, plus the rounding of the logit to fp32.
+constexpr float kRtBound = (8 + 1) * 0x1p-24f * 1.02f;
 
 // LDS written and read by lanes of one wavefront
 __device__ __forceinline__ void wave_lds_fence() {
@@ -44,237 +46,422 @@ template <typename T, typename F> __device__ __forceinline__ T row_reduce(T v, F
   v = f(v, dpp<0x141>(v));   // half-row mirror
   return f(v, dpp<0x140>(v));
 }
-__device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ double max_of(double a, double b) { return fmax(a, b); }
-template <typename T> __device__ __forceinline__ T row_max(T v) { return row_reduce(v, [](T a, T b) { return max_of(a, b); }); }
-template <typename T> __device__ __forceinline__ T row_min(T v) { return -row_max(-v); }
-template <typename T> __device__ __forceinline__ T row_sum(T v) { return row_reduce(v, [](T a, T b) { return a + b; }); }
+__device__ __forceinline__ int row_max(int v) { return row_reduce(v, [](int a, int b) { return max(a, b); }); }
+__device__ __forceinline__ int row_min(int v) { return row_reduce(v, [](int a, int b) { return min(a, b); }); }
 __device__ __forceinline__ int row_or(int v) { return row_reduce(v, [](int a, int b) { return a | b; }); }
-__device__ __forceinline__ int row_min_int(int v) { return row_reduce(v, [](int a, int b) { return min(a, b); }); }
-__device__ __forceinline__ float exp_of(float v) { return expf(v); }
-__device__ __forceinline__ double exp_of(double v) { return exp(v); }
-__device__ __forceinline__ float abs_of(float v) { return fabsf(v); }
-__device__ __forceinline__ double abs_of(double v) { return fabs(v); }
-template <typename R> constexpr R lowest_of() { return sizeof(R) == 8 ? static_cast<R>(-DBL_MAX) : static_cast<R>(-FLT_MAX); }
+__device__ __forceinline__ float row_max(float v) { return row_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ double row_max(double v) { return row_reduce(v, [](double a, double b) { return fmax(a, b); }); }
+template <typename T> __device__ __forceinline__ T row_sum(T v) { return row_reduce(v, [](T a, T b) { return a + b; }); }
+__device__ __forceinline__ double wave_max(double v) {
+  v = row_max(v);
+  v = fmax(v, __shfl_xor(v, 16, kWave));
+  return fmax(v, __shfl_xor(v, 32, kWave));
+}
+__device__ __forceinline__ double wave_add(double v) {
+  v = row_sum(v);
+  v += __shfl_xor(v, 16, kWave);
+  return v + __shfl_xor(v, 32, kWave);
+}
+__device__ __forceinline__ double wave_min(double v) { return -wave_max(-v); }
 
-// Selection for one token by the 16 lanes of a DPP row; lane s has the experts s + 16 v.
-//   R = float : all keys in fp32 from logits that are off by at most `tol`; returns in every lane of the row whether two keys
-//               are too close for that
-//   R = double: the same on fp64 keys; bit v of `exact`: the logit of the lane's expert is settled.  `again` gets the experts
-//               (bit v) whose logits have to be settled, 0 in every lane of the row: the selection is final
-// The selected experts go to sel[0 .. k) (the caller has filled it with -1), lowest index first among equal keys.
-// sc: scores of the lane's experts, shift and total: softmax is exp(l - shift) / total.
+// Hardware exp2: a few units of 2^-24
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.44269504f); }
+// fp32 values as integers of the same order, and back; kNoKey is below all of them
+constexpr int kNoKey = INT_MIN;
+__device__ __forceinline__ int order_of(float v) {
+  const int b = __float_as_int(v);
+  return b ^ ((b >> 31) & 0x7FFFFFFF);
+}
+__device__ __forceinline__ float value_of(int o) { return __int_as_float(o ^ ((o >> 31) & 0x7FFFFFFF)); }
+
+__device__ __forceinline__ bool keys_are_logits(const RouteArgs& a) { return a.bias == nullptr && !(a.n_groups > 1 && a.group_top == 2); }
+
+// How far a key may be off where the logits are off by tol: the score's slope is at most a quarter (sigmoid) or twice the score
+// (softmax).  Not for large tol, where a slope says nothing.
+__device__ __forceinline__ float key_tolerance(const RouteArgs& a, float tol) {
+  if (keys_are_logits(a)) return tol;
+  return tol < 0.05f ? (a.sigmoid ? 0.25f : 2.2f) * tol : INFINITY;
+}
 template <typename R>
-__device__ __forceinline__ bool route_select(const RouteArgs& a, const double* l_row, R* key_row, R* grp_row, volatile int* sel, float tol, int exact, int* again,
-                                             float (&sc)[4], float& shift, float& total) {
-  constexpr bool kExact = sizeof(R) == 8;
-  const int s = threadIdx.x & 15, E = a.E;
-  const R kNone = -INFINITY;
+__device__ __forceinline__ bool near_keys(R x, R y, float width, R slack) {
+  return !(fabs(x - y) > static_cast<R>(width) + slack * (fabs(x) + fabs(y)));
+}
+
+// Scores of one token by the 16 lanes of a DPP row, lane s: experts s + 16 v.  Softmax is exp(l - shift) / total.
+__device__ __forceinline__ void route_scores(const RouteArgs& a, const double* l_row, float (&sc)[4], double& shift, float& total) {
+  const int s = threadIdx.x & 15;
   double l[4];
-  R key[4], score[4];
-  float mx = -INFINITY;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    l[v] = s + 16 * v < E ? l_row[s + 16 * v] : static_cast<double>(-INFINITY);
-    mx = fmaxf(mx, static_cast<float>(l[v]));
-  }
-  const bool by_logit = a.bias == nullptr && !(a.n_groups > 1 && a.group_top == 2);
+  for (int v = 0; v < 4; ++v) l[v] = s + 16 * v < a.E ? l_row[s + 16 * v] : static_cast<double>(-INFINITY);
+  shift = 0.0;
   total = 1.0f;
   if (a.sigmoid) {
-    shift = 0.0f;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      score[v] = s + 16 * v < E ? R(1) / (R(1) + exp_of(static_cast<R>(-l[v]))) : R(0);
-      sc[v] = static_cast<float>(score[v]);
-    }
+    for (int v = 0; v < 4; ++v) sc[v] = __builtin_amdgcn_rcpf(1.0f + exp_of(static_cast<float>(-l[v])));
   } else {
-    mx = row_max(mx);
-    shift = mx;
-    R sum = 0;
+    shift = row_max(fmax(fmax(l[0], l[1]), fmax(l[2], l[3])));
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      score[v] = s + 16 * v < E ? exp_of(static_cast<R>(l[v] - static_cast<double>(mx))) : R(0);
-      sum += score[v];
-    }
-    sum = row_sum(sum);
-    total = static_cast<float>(sum);
+    for (int v = 0; v < 4; ++v) sc[v] = exp_of(static_cast<float>(l[v] - shift));
+    total = row_sum((sc[0] + sc[1]) + (sc[2] + sc[3]));
+    const float inv = __builtin_amdgcn_rcpf(total);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      score[v] /= sum;
-      sc[v] = static_cast<float>(score[v]);
-    }
+    for (int v = 0; v < 4; ++v) sc[v] *= inv;
   }
-  // how far a key may be off: the logits' bound through the score's slope (a quarter for the sigmoid, at most 2 P for the softmax)
-  // and, in fp32, the rounding of the score
-  float delta = tol;
-  if (!by_logit) {
-    delta = a.sigmoid ? 0.25f * tol : 2.2f * tol;
-    if (!kExact) delta += (a.sigmoid ? 8.0f : 16.0f + 4.0f * fabsf(mx)) * 0x1p-24f;
-    if (!(tol < 0.05f)) delta = INFINITY;
-  }
-  const R slack = kExact ? R(0x1p-50) : R(4 * 0x1p-24);
-  auto near = [&](R x, R y, float width) { return !(abs_of(x - y) > static_cast<R>(width) + slack * (abs_of(x) + abs_of(y))); };
+#pragma unroll
+  for (int v = 0; v < 4; ++v)
+    if (s + 16 * v >= a.E) sc[v] = 0.0f;
+}
+
+// Selection for one token by the 16 lanes of a DPP row, on fp32 keys; the selected experts go to sel[0 .. k), which the caller
+// has filled with -1.  Returns the experts (bit v: s + 16 v) whose logits have to be settled because keys that decide are
+// too close: logits are off by `tol`, scores by the rounding of exp_of and rcp.  Bit 4: groups or equal keys are among them.
+// key_row, grp_row: 64 integers of LDS each (groups only), m_row: 8.
+__device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_row, const float (&sc)[4], double shift, int* key_row, int* grp_row,
+                                            int* m_row, int* sel, float tol) {
+  const int s = threadIdx.x & 15, E = a.E;
+  const bool by_logit = keys_are_logits(a);
+  float delta = key_tolerance(a, tol);
+  if (!by_logit) delta += (a.sigmoid ? 8.0f : 16.0f + 4.0f * fabsf(static_cast<float>(shift))) * 0x1p-24f;
+  const float slack = 4 * 0x1p-24f;
+  int key[4];
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     const int e = s + 16 * v;
-    key[v] = kNone;
-    if (e < E) {
-      key[v] = by_logit ? static_cast<R>(l[v]) : score[v] + (a.bias ? static_cast<R>(a.bias[e]) : R(0));
-      if (key[v] != key[v]) key[v] = lowest_of<R>();
-    }
+    float f = -INFINITY;
+    if (e < E) f = by_logit ? static_cast<float>(l_row[e]) : sc[v] + (a.bias ? a.bias[e] : 0.0f);
+    if (f != f) f = -FLT_MAX;
+    key[v] = f > -INFINITY ? order_of(f) : kNoKey;
   }
-  bool close = false;
+  bool close = false, grouped = false;
   int more = 0;
   if (a.n_groups > 1) {
     const int G = a.n_groups, n = E / G;
 #pragma unroll
-    for (int v = 0; v < 4; ++v)
-      if (s + 16 * v < E) key_row[s + 16 * v] = key[v];
+    for (int v = 0; v < 4; ++v) key_row[s + 16 * v] = key[v];
     wave_lds_fence();
-    R gs[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    int worst_in = INT_MAX, best_out = kNoKey;
+    uint64_t open = 0;
+#pragma unroll 1
+    for (int i = 0; 16 * i < G; ++i) {
       const int g = s + 16 * i;
-      gs[i] = kNone;
-      if (g < G) {
-        R t1 = kNone, t2 = kNone;
-        for (int j = 0; j < n; ++j) {
-          const R kv = key_row[g * n + j];
-          t2 = max_of(t2, kv > t1 ? t1 : kv);
-          t1 = max_of(t1, kv);
+      int t1 = kNoKey, t2 = kNoKey;
+#pragma unroll 1
+      for (int j = 0; j < n; j += 8) {
+        int kv[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) kv[q] = key_row[min(g * n + min(j + q, n - 1), 63)];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const int c = j + q < n ? kv[q] : kNoKey;
+          t2 = max(t2, min(c, t1));
+          t1 = max(t1, c);
         }
-        gs[i] = a.group_top == 2 ? t1 + t2 : t1;
-        grp_row[g] = gs[i];
       }
+      int gs = t1;
+      if (a.group_top == 2) gs = t2 == kNoKey ? kNoKey : order_of(value_of(t1) + value_of(t2));
+      if (g < G) grp_row[g] = gs;
     }
     wave_lds_fence();
-    uint64_t open = 0;
-    R worst_in = INFINITY, best_out = kNone;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (16 * i >= G) break;
-      const int g = s + 16 * i;
+#pragma unroll 1
+    for (int i = 0; 16 * i < G; ++i) {
+      const int g = s + 16 * i, gs = grp_row[min(g, G - 1)];
       int rank = 0;
-      for (int j = 0; j < G; ++j) {
-        const R o = grp_row[j];
-        rank += (o > gs[i] || (o == gs[i] && j < g)) ? 1 : 0;
+#pragma unroll 1
+      for (int j = 0; j < G; j += 8) {
+        int o[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) o[q] = grp_row[min(j + q, G - 1)];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) rank += j + q < G && (o[q] > gs || (o[q] == gs && j + q < g)) ? 1 : 0;
       }
       const bool in = g < G && rank < a.top_groups;
       if (g < G) {
-        if (in) worst_in = -max_of(-worst_in, -gs[i]);
-        else best_out = max_of(best_out, gs[i]);
+        if (in) worst_in = min(worst_in, gs);
+        else best_out = max(best_out, gs);
       }
       open |= ((__ballot(in) >> (threadIdx.x & 48)) & 0xFFFFull) << (16 * i);
     }
     worst_in = row_min(worst_in);
     best_out = row_max(best_out);
     const float width = 2.0f * static_cast<float>(a.group_top) * delta;
-    if (best_out > kNone && near(worst_in, best_out, width)) {
-      if constexpr (kExact) {   // every unsettled expert of the groups around the border
+    const unsigned inv_n = 65536u / static_cast<unsigned>(n) + 1u;   // e / n for e < 64
+    if (best_out != kNoKey && near_keys(value_of(worst_in), value_of(best_out), width, slack)) {   // the groups around the border
+      close = grouped = true;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int e = s + 16 * v;
-          if (e < E && !(exact >> v & 1)) {
-            const R g = grp_row[e / n];
-            if (near(g, worst_in, width) || near(g, best_out, width)) more |= 1 << v;
-          }
+      for (int v = 0; v < 4; ++v)
+        if (s + 16 * v < E) {
+          const float g = value_of(grp_row[((s + 16 * v) * inv_n) >> 16]);
+          if (near_keys(g, value_of(worst_in), width, slack) || near_keys(g, value_of(best_out), width, slack)) more |= 1 << v;
         }
-      } else {
-        close = true;
-      }
     }
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int e = s + 16 * v;
-      if (e < E && !((open >> (e / n)) & 1)) key[v] = kNone;
-    }
+    for (int v = 0; v < 4; ++v)
+      if (!((open >> (((s + 16 * v) * inv_n) >> 16)) & 1)) key[v] = kNoKey;
   }
-  R first[4];
+  int first[4];
 #pragma unroll
   for (int v = 0; v < 4; ++v) first[v] = key[v];
-  R last = INFINITY;
-  int surplus = 0;   // keys taken less rounds: equal keys are close
+  // a lane's keys in descending order, their experts in the bytes of ex
+  int ex = s | (s + 16) << 8 | (s + 32) << 16 | (s + 48) << 24;
+  auto order = [&](int i, int j) __attribute__((always_inline)) {
+    const bool swap = key[j] > key[i];
+    const int ki = swap ? key[j] : key[i], kj = swap ? key[i] : key[j];
+    const int bi = (ex >> (8 * i)) & 0xFF, bj = (ex >> (8 * j)) & 0xFF, x = swap ? bi ^ bj : 0;
+    key[i] = ki;
+    key[j] = kj;
+    ex ^= x << (8 * i) | x << (8 * j);
+  };
+  order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
+  float last = INFINITY;
+  int surplus = 0;   // keys taken less rounds: equal keys of several lanes go together, and are close
+#pragma unroll 1
   for (int j = 0; j <= a.k; ++j) {
-    const R m = row_max(max_of(max_of(key[0], key[1]), max_of(key[2], key[3])));
-    if constexpr (kExact) {
-      if (j == a.k) break;
-      int e_min = 64;
-#pragma unroll
-      for (int v = 3; v >= 0; --v)
-        if (key[v] == m && m > kNone) e_min = s + 16 * v;
-      e_min = row_min_int(e_min);
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        if (e_min == s + 16 * v) {
-          sel[j] = e_min;
-          key[v] = kNone;
-        }
-      if (m > kNone) {   // unsettled experts whose key may be on the other side of this one
-        int count = 0, open = 0;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-          if (first[v] > kNone && near(first[v], m, 2.0f * delta)) {
-            ++count;
-            if (!(exact >> v & 1)) open |= 1 << v;
-          }
-        if (row_sum(count) > 1) more |= open;
-      }
-    } else {
-      if (j > 0 && m > kNone && near(last, m, 2.0f * delta)) close = true;
-      last = m;
-      surplus -= m > kNone && s == 0 ? 1 : 0;
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        if (key[v] == m && m > kNone) {   // equal keys go together
-          if (j < a.k) sel[j] = s + 16 * v;
-          key[v] = kNone;
-          ++surplus;
-        }
+    const int m = row_max(key[0]);
+    const float mv = value_of(m);
+    const bool some = m != kNoKey, hit = some && key[0] == m;
+    close |= some && j > 0 && near_keys(last, mv, 2.0f * delta, slack);
+    last = mv;
+    surplus += (hit ? 1 : 0) - (some && s == 0 ? 1 : 0);
+    if (hit && j < a.k) {
+      sel[j] = ex & 0xFF;
+      m_row[j] = m;
     }
+    key[0] = hit ? key[1] : key[0];
+    key[1] = hit ? key[2] : key[1];
+    key[2] = hit ? key[3] : key[2];
+    key[3] = hit ? kNoKey : key[3];
+    ex = hit ? ex >> 8 : ex;
   }
-  if constexpr (!kExact) close |= row_sum(surplus) > 0;
-  if constexpr (kExact) *again = more;
-  return close;
+  close |= row_sum(surplus) > 0;
+  if (__ballot(close)) {   // rare
+    wave_lds_fence();
+#pragma unroll 1
+    for (int j = 0; j < a.k; ++j) {   // experts whose key may lie on the other side of a selected one, itself included
+      const int m = m_row[j];
+      int count = 0, at = 0;
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        if (close && sel[j] >= 0 && first[v] != kNoKey && near_keys(value_of(first[v]), value_of(m), 2.0f * delta, slack)) {
+          ++count;
+          at |= 1 << v;
+        }
+      if (row_sum(count) > 1) more |= at;
+    }
+    if (grouped || row_sum(surplus) > 0) more |= 16;
+  }
+  return more;
 }
 
-// fp64 logits of the experts e0, e1 of a token by one wavefront.
-__device__ __forceinline__ void exact_logits(const RouteArgs& a, int tok, int e0, int e1, double* l_row) {
-  const int lane = threadIdx.x & 63;
-  const uint16_t* const xr = a.x + static_cast<int64_t>(tok) * a.d;
-  double s0 = 0.0, s1 = 0.0;
-#pragma unroll 8
-  for (int c = lane; c < a.d; c += 64) {
-    const double xv = bf16_to_f32(xr[c]);
-    s0 = fma(xv, static_cast<double>(bf16_to_f32(a.w_router[c * a.E + e0])), s0);
-    s1 = fma(xv, static_cast<double>(bf16_to_f32(a.w_router[c * a.E + e1])), s1);
+// The same for one token by a whole wavefront (lane e: expert e), on fp64 keys: the rare case, compact rather than fast.
+// exact: bit e, the logit of expert e is settled; the others are off by tol.  Returns the experts whose logits have to be
+// settled for the selection to be that of fp64 logits (0: it is final, sel is written).
+__device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const double* l_row, double* key_row, double* grp_row, int* sel, float tol,
+                                                       uint64_t exact) {
+  const int e = threadIdx.x & 63, E = a.E;
+  const double kNone = -INFINITY, slack = 0x1p-50;
+  const float width = 2.0f * key_tolerance(a, tol);
+  const double l = e < E ? l_row[e] : kNone;
+  double key = l;
+  if (!keys_are_logits(a)) {
+    if (a.sigmoid) {
+      key = 1.0 / (1.0 + exp(-l));
+    } else {
+      key = exp(l - wave_max(l));
+      if (e >= E) key = 0.0;
+      key /= wave_add(key);
+    }
+    if (a.bias && e < E) key += static_cast<double>(a.bias[e]);
   }
-  s0 = wave_sum(s0);
-  s1 = wave_sum(s1);
-  if (lane == 0) {
-    l_row[e0] = s0;
-    l_row[e1] = s1;
+  if (key != key) key = -DBL_MAX;
+  if (e >= E) key = kNone;
+  uint64_t more = 0;
+  if (a.n_groups > 1) {
+    const int G = a.n_groups, n = E / G;
+    key_row[e] = key;
+    wave_lds_fence();
+    double t1 = kNone, t2 = kNone;
+    if (e < G)
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const double kv = key_row[e * n + j];
+        t2 = fmax(t2, fmin(kv, t1));
+        t1 = fmax(t1, kv);
+      }
+    const double gs = a.group_top == 2 ? t1 + t2 : t1;
+    grp_row[e] = gs;
+    wave_lds_fence();
+    int rank = 0;
+#pragma unroll 1
+    for (int j = 0; j < G; ++j) {
+      const double o = grp_row[j];
+      rank += (o > gs || (o == gs && j < e)) ? 1 : 0;
+    }
+    const uint64_t open = __ballot(e < G && rank < a.top_groups);
+    const double worst_in = wave_min(e < G && rank < a.top_groups ? gs : INFINITY), best_out = wave_max(e < G && rank >= a.top_groups ? gs : kNone);
+    const double mine = grp_row[min(e / n, G - 1)];
+    const float w = width * static_cast<float>(a.group_top);
+    if (best_out > kNone && near_keys(worst_in, best_out, w, slack))   // the groups around the border
+      more |= __ballot(e < E && (near_keys(mine, worst_in, w, slack) || near_keys(mine, best_out, w, slack)));
+    if (e < E && !((open >> (e / n)) & 1)) key = kNone;
   }
+  const double first = key;
+  int got = -1;
+#pragma unroll 1
+  for (int j = 0; j < a.k; ++j) {
+    const double m = wave_max(key);
+    if (!(m > kNone)) break;
+    const int win = __builtin_ctzll(__ballot(key == m));   // lowest index among equal keys
+    if (e == j) got = win;
+    if (e == win) key = kNone;
+    // experts whose key may lie on the other side of this one, itself included
+    const uint64_t at = __ballot(first > kNone && near_keys(first, m, width, slack));
+    if (__builtin_popcountll(at) > 1) more |= at;
+  }
+  if (e < 8) sel[e] = got;
+  return more & ~exact;
 }
 
 struct RouteLds {
   union {
-    double red[4][32 * 64];                    // partial sums of four wavefronts: one lane's 32 logits in stride
+    struct {
+      unsigned char w[kRtWaves][kRtUnit * 128 + 128];  // a unit of router rows of each wavefront (columns beyond E of the last row are read, never used)
+      unsigned char x[kRtWaves][kRtTokens * 128];      // and of the tokens
+    } stage;
+    double red[kRtWaves][32 * 64];                     // partial sums: the 32 (16) of a lane in stride
     struct {
       double key[kRtTokens][kRtRow], grp[kRtTokens][kRtRow];
+      int m[kRtTokens][8];
+      int pairs[kRtTokens * 64];                       // logits to settle: token << 6 | expert
+      double sum[kRtWaves][64], part[2][kRtWaves];
     } pick;
   };
   double l[kRtTokens][kRtRow];                 // finished logits
-  float nx[kRtWaves][64], nw[kRtWaves][2][64]; // shares of |x|^2 of the tokens and of |w|^2 of the experts
-  uint32_t orx[kRtWaves][64], orw[kRtWaves];   // bits of the values: all zero or not
+  float nx[kRtWaves][kRtTokens], nw[kRtWaves][128]; // shares of |x|^2 of the tokens and of |w|^2 of the experts (two each)
+  uint32_t orx[kRtWaves][kRtTokens], orw[kRtWaves]; // bits of the values: all zero or not
+  float x2[kRtTokens], w2;                     // |x|^2, the largest |w|^2; 0: nothing but zeros
   int sel[kRtTokens][8];
-  double sum[kRtWaves][64];
   int cnt[64];
+  int n_pairs;
 };
+static_assert(sizeof(RouteLds) <= 160 * 1024, "LDS of a CU");
 
-// 64 channels of the 32 tokens and of all experts
+// The router's weights as the operands of route_kernel: for a unit of 64 channels, operand f of step s is 64 lanes of 16
+// bytes, lane 32 g + r: channels 16 s + 8 g .. + 7 of expert r (NF = 1, E <= 32) or 2 r + f (NF = 2).  And as columns [E, d],
+// for logits that are settled (reading them out of the operands, a line of memory for 16 bytes, took 13000 cycles for two).
+// One unit per workgroup, which also leaves every expert's share of |w|^2 and the bits of its values.
+template <int NF>
+__global__ __launch_bounds__(256) void route_layout_kernel(const uint16_t* __restrict__ w, int d, int E, u4* __restrict__ ops, u4* __restrict__ cols,
+                                                           float* __restrict__ w2, uint32_t* __restrict__ bits) {
+  __shared__ uint16_t s_w[kRtUnit][64 + 2];
+  __shared__ float s_n[4][64];
+  __shared__ uint32_t s_any[4][64];
+  const int u = blockIdx.x, tid = threadIdx.x, e = tid & 63, part = tid >> 6;
+  const uint16_t* const src = w + static_cast<int64_t>(u) * kRtUnit * E;
+  uint16_t v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = e < E ? src[(16 * part + i) * E + e] : 0;
+  float n = 0.0f;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    s_w[16 * part + i][e] = v[i];
+    n = fmaf(bf16_to_f32(v[i]), bf16_to_f32(v[i]), n);
+    any |= v[i] & 0x7FFFu;
+  }
+  s_n[part][e] = n;
+  s_any[part][e] = any;
+  __syncthreads();
+  auto piece = [&](int c, int col) {   // channels c .. c + 7 of an expert
+    u4 o;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] = s_w[c + 2 * q][col] | static_cast<uint32_t>(s_w[c + 2 * q + 1][col]) << 16;
+    return o;
+  };
+#pragma unroll
+  for (int i = tid; i < 4 * NF * 64; i += 256) {
+    const int lane = i & 63, f = (i >> 6) % NF, s = (i >> 6) / NF;
+    ops[static_cast<int64_t>(u) * 4 * NF * 64 + i] = piece(16 * s + 8 * (lane >> 5), NF == 2 ? 2 * (lane & 31) + f : lane & 31);
+  }
+#pragma unroll
+  for (int i = tid; i < 8 * 64; i += 256)
+    if (i >> 3 < E) cols[static_cast<int64_t>(i >> 3) * (d >> 3) + u * 8 + (i & 7)] = piece(8 * (i & 7), i >> 3);
+  if (tid < 64) {
+    w2[u * 64 + tid] = (s_n[0][tid] + s_n[1][tid]) + (s_n[2][tid] + s_n[3][tid]);
+    bits[u * 64 + tid] = s_any[0][tid] | s_any[1][tid] | s_any[2][tid] | s_any[3][tid];
+  }
+}
+
+// fp64 logits of the listed pairs by the whole workgroup, two at a time (mostly the two of one token).  Code that a workgroup
+// in fifty reaches is fetched from memory when it does: here and below it is short rather than unrolled.
+template <bool LAID>
+__device__ __forceinline__ void settle_logits(const RouteArgs& a, int t0, RouteLds& lds) {
+  const int tid = threadIdx.x, n = lds.n_pairs;
+#pragma unroll 1
+  for (int at = 0; at < n; at += 2) {
+    double s[2] = {0.0, 0.0};
+#pragma unroll 1
+    for (int c = 8 * tid; c < a.d; c += 8 * kRtThreads) {
+      u4 x[2], w[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int p = lds.pick.pairs[min(at + i, n - 1)], e = p & 63;
+        x[i] = *reinterpret_cast<const u4*>(a.x + static_cast<int64_t>(t0 + (p >> 6)) * a.d + c);
+        if constexpr (LAID) {
+          w[i] = a.cols[(static_cast<int64_t>(e) * a.d + c) >> 3];
+        } else {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            w[i][q] = a.w_router[static_cast<size_t>(c + 2 * q) * a.E + e] | static_cast<uint32_t>(a.w_router[static_cast<size_t>(c + 2 * q + 1) * a.E + e]) << 16;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          s[i] = fma(static_cast<double>(bf16_lo(x[i][q])), static_cast<double>(bf16_lo(w[i][q])), s[i]);
+          s[i] = fma(static_cast<double>(bf16_hi(x[i][q])), static_cast<double>(bf16_hi(w[i][q])), s[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s[i] = wave_add(s[i]);
+      if ((tid & 63) == 0) lds.pick.part[i][tid >> 6] = s[i];
+    }
+    __syncthreads();
+    if (tid < 2 && at + tid < n) {
+      double sum = 0.0;
+#pragma unroll 1
+      for (int i = 0; i < kRtWaves; ++i) sum += lds.pick.part[tid][i];
+      const int p = lds.pick.pairs[at + tid];
+      lds.l[p >> 6][p & 63] = sum;
+    }
+    __syncthreads();
+  }
+}
+
+// Puts the two experts of a token that were too close into their order: e0 < e1, settled; lane 0 and lane 1 of the wavefront
+// have one each.  Both are selected or one of them is.  Keys are logits or sigmoid scores: softmax scores of a row have a
+// denominator, which takes route_select_exact.
+__device__ __forceinline__ void order_two(const RouteArgs& a, const double* l_row, int* sel, int e0, int e1) {
+  const int lane = threadIdx.x & 63, e = lane == 0 ? e0 : e1;
+  double key = l_row[e];
+  if (!keys_are_logits(a)) {
+    key = 1.0 / (1.0 + exp(-key));
+    if (a.bias) key += static_cast<double>(a.bias[e]);
+  }
+  const double other = __shfl(key, 1, kWave);
+  const bool keep = __builtin_amdgcn_readlane(key >= other, 0);   // lane 0: e0 in front of e1
+  const int mine = lane < a.k ? sel[lane] : -1;
+  const uint64_t at = __ballot(mine == e0 || mine == e1);
+  const int win = keep ? e0 : e1, lose = keep ? e1 : e0;
+  if (at >> lane & 1) sel[lane] = (at & ((1ull << lane) - 1)) == 0 ? win : lose;
+}
+
+// 64 channels of the 32 tokens and the router's rows of these channels: operands (LAID) or the rows as they lie in memory
+template <int NL>
 struct RouteUnit {
   u4 x[4];
-  uint32_t w[32];
+  u4 w[NL];
 };
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -282,195 +469,275 @@ __device__ __forceinline__ float dot2(uint32_t v, float c) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v), __builtin_bit_cast(bf16x2, v), c, false);
 }
 
-// PAIRS: E is even, two experts of a row are one aligned word.
-template <bool PAIRS>
+// LAID: the router's weights come as operands, from route_layout_kernel.  Otherwise (a few tokens: one launch) the rows of a
+// unit come as they lie in memory, NL loads of 16 bytes a lane (8 NL >= E), and are turned into the operands of NF = 2 through
+// LDS.  PAIRS: E is even, two experts of a row are one aligned word.  (Loading those words from memory takes the
+// address unit as long for four bytes as for 16: 580 cycles a unit, of 36 loads instead of 12.)
+template <int NF, bool LAID, int NL, bool PAIRS>
 __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
-  __shared__ RouteLds lds;
+  __shared__ __attribute__((aligned(16))) RouteLds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r = lane & 31, g = lane >> 5;
   const int t0 = blockIdx.x * kRtTokens;
-  const int units = a.d / kRtUnit;
+  // neighbouring units go to one wavefront: at any time the eight read places of a row that lie far apart (rows are often a
+  // multiple of 4096 bytes, and so are the places of one memory channel)
+  const int units = a.d / kRtUnit, u_begin = wave * units / kRtWaves, u_end = (wave + 1) * units / kRtWaves;
   if (tid < 64) lds.cnt[tid] = 0;
   if (tid < kRtTokens * 8) lds.sel[tid >> 3][tid & 7] = -1;
 
-  const uint16_t* const xr = a.x + static_cast<int64_t>(min(t0 + r, a.T - 1)) * a.d + 8 * g;
-  const unsigned row_bytes = 2u * a.E;
-  const int e_lo = PAIRS ? 2 * min(r, a.E / 2 - 1) : min(2 * r, a.E - 1), e_hi = min(2 * r + 1, a.E - 1);
+  // 16-byte pieces of the tokens' units: eight lanes read the 128 bytes of a token, piece p of token t goes to place p ^ (t & 7) of
+  // its 128 bytes of LDS, which spreads the operand reads (32 tokens, one piece) over the banks.  (Operands straight from memory
+  // touch the 32 rows four times each: 8192 x 2048 50000 cycles instead of 23000 up to the logits.)
+  const uint32_t x_bytes = 2u * a.d;
+  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.x) + static_cast<int64_t>(t0) * a.d, 0,
+                                                                      static_cast<int>(min(a.T - t0, kRtTokens) * x_bytes), 0x00020000);   // zeros behind the last token
+  const int x_lane = static_cast<int>((lane >> 3) * x_bytes) + 16 * (lane & 7);
+  const uint32_t row_bytes = 2u * a.E;
+  const __amdgpu_buffer_rsrc_t rw = LAID ? __builtin_amdgcn_make_buffer_rsrc(const_cast<u4*>(a.ops), 0, units * 4 * NF * 1024, 0x00020000)
+                                         : __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.w_router), 0, static_cast<int>(a.d * row_bytes), 0x00020000);
   auto load = [&](int u) __attribute__((always_inline)) {
-    RouteUnit q;
-    u = min(u, units - 1);
+    RouteUnit<NL> q;
+    u = min(u, u_end - 1);
+    const uint32_t base = static_cast<uint32_t>(u) * (LAID ? 4u * NF * 1024u : kRtUnit * row_bytes);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) q.x[s] = *reinterpret_cast<const u4*>(xr + u * kRtUnit + 16 * s);
-    const char* const wb = reinterpret_cast<const char*>(a.w_router) + static_cast<size_t>(u) * kRtUnit * row_bytes;   // uniform
-    const unsigned lo = 8u * g * row_bytes + 2u * e_lo, hi = 8u * g * row_bytes + 2u * e_hi;
+    for (int i = 0; i < NL; ++i) q.w[i] = __builtin_amdgcn_raw_buffer_load_b128(rw, 16 * lane + 1024 * i, base, 0);   // zeros behind the last row
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const char* const p = wb + (16 * s + i) * row_bytes;
-        if constexpr (PAIRS) q.w[8 * s + i] = *reinterpret_cast<const uint32_t*>(p + lo);
-        else q.w[8 * s + i] = *reinterpret_cast<const uint16_t*>(p + lo) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p + hi)) << 16;
-      }
+    for (int i = 0; i < 4; ++i) q.x[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, x_lane, static_cast<uint32_t>(8 * i) * x_bytes + 2u * kRtUnit * u, 0);
+    __builtin_amdgcn_sched_barrier(0);   // the loads of a unit leave before the work on the one in front of it
     return q;
   };
-  double even[16], odd[16];
+  unsigned char* const stage = lds.stage.w[wave];
+  const unsigned char* const col = stage + 8 * g * row_bytes + 4 * r;   // experts 2 r, 2 r + 1 of row 8 g; beyond E what lies there
+  double acc[NF][16];
 #pragma unroll
-  for (int v = 0; v < 16; ++v) even[v] = odd[v] = 0.0;
-  float nx = 0.0f, nw0 = 0.0f, nw1 = 0.0f;
-  uint32_t orx = 0, orw = 0;
-  auto compute = [&](const RouteUnit& q) __attribute__((always_inline)) {
-    v16f c0, c1;
+  for (int f = 0; f < NF; ++f)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) c0[v] = c1[v] = 0.0f;
+    for (int v = 0; v < 16; ++v) acc[f][v] = 0.0;
+  float nx[4] = {}, nw[NF] = {};   // nx, orx: tokens 8 i + lane / 8
+  uint32_t orx[4] = {}, orw = 0;
+  unsigned char* const x_stage = lds.stage.x[wave];
+  const unsigned char* const x_row = x_stage + r * 128;
+  auto compute = [&](const RouteUnit<NL>& q) __attribute__((always_inline)) {
+    if constexpr (!LAID) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        *reinterpret_cast<u4*>(stage + 1024 * i + 16 * lane) = q.w[i];
+        orw |= q.w[i].x | q.w[i].y | q.w[i].z | q.w[i].w;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      *reinterpret_cast<u4*>(x_stage + (8 * i + (lane >> 3)) * 128 + 16 * ((lane & 7) ^ (lane >> 3))) = q.x[i];
+      nx[i] = dot2(q.x[i].x, dot2(q.x[i].y, dot2(q.x[i].z, dot2(q.x[i].w, nx[i]))));
+      orx[i] |= q.x[i].x | q.x[i].y | q.x[i].z | q.x[i].w;
+    }
+    wave_lds_fence();
+    v16f c[NF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) c[f][v] = 0.0f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      u4 b0, b1;
+      const u4 x = *reinterpret_cast<const u4*>(x_row + 16 * ((2 * s + g) ^ (r & 7)));
+      u4 b[NF];
+      if constexpr (LAID) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        b0[i] = __builtin_amdgcn_perm(q.w[8 * s + 2 * i + 1], q.w[8 * s + 2 * i], 0x05040100u);
-        b1[i] = __builtin_amdgcn_perm(q.w[8 * s + 2 * i + 1], q.w[8 * s + 2 * i], 0x07060302u);
-        nx = dot2(q.x[s][i], nx);
-        nw0 = dot2(b0[i], nw0);
-        nw1 = dot2(b1[i], nw1);
-        orx |= q.x[s][i];
-        orw |= b0[i] | b1[i];
+        for (int f = 0; f < NF; ++f) b[f] = q.w[NF * s + f];
+      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const unsigned char* const p = col + (16 * s + i) * row_bytes;
+          if constexpr (PAIRS) w[i] = *reinterpret_cast<const uint32_t*>(p);
+          else w[i] = *reinterpret_cast<const uint16_t*>(p) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(p + 2)) << 16;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          b[0][i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
+          b[1][i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+          nw[0] = dot2(b[0][i], nw[0]);
+          nw[1] = dot2(b[1][i], nw[1]);
+        }
       }
-      c0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q.x[s]), __builtin_bit_cast(bf16x8, b0), c0, 0, 0, 0);
-      c1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, q.x[s]), __builtin_bit_cast(bf16x8, b1), c1, 0, 0, 0);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) c[f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, b[f]), c[f], 0, 0, 0);
     }
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      even[v] += static_cast<double>(c0[v]);
-      odd[v] += static_cast<double>(c1[v]);
-    }
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[f][v] += static_cast<double>(c[f][v]);
+    wave_lds_fence();
   };
-  if (wave < units) {
-    RouteUnit p = load(wave), q;
-    for (int u = wave; u < units; u += 2 * kRtWaves) {
-      q = load(u + kRtWaves);
+  float op_n = 0.0f;   // LAID: this wavefront's share of the units' |w|^2 of expert `lane`
+  uint32_t op_any = 0;
+  if constexpr (LAID)
+    for (int u = wave; u < units; u += kRtWaves) {
+      op_n += a.op_w2[u * 64 + lane];
+      op_any |= a.op_bits[u * 64 + lane];
+    }
+  if (u_begin < u_end) {
+    RouteUnit<NL> p = load(u_begin), q;
+#pragma unroll 1
+    for (int u = u_begin; u < u_end; u += 2) {
+      q = load(u + 1);
       compute(p);
-      if (u + kRtWaves >= units) break;
-      p = load(u + 2 * kRtWaves);
+      if (u + 1 >= u_end) break;
+      p = load(u + 2);
       compute(q);
     }
   }
-  // Sums over the wavefronts in a fixed order: 4 .. 7 onto 0 .. 3, then all four.  Element v of a lane is token
-  // (v & 3) + 8 (v >> 2) + 4 g, experts 2 r (even) and 2 r + 1 (odd).
-  lds.nx[wave][lane] = nx;
-  lds.nw[wave][0][lane] = nw0;
-  lds.nw[wave][1][lane] = nw1;
-  lds.orx[wave][lane] = orx & 0x7FFF7FFFu;
-  const bool any_w = __ballot((orw & 0x7FFF7FFFu) != 0) != 0;
-  if (lane == 0) lds.orw[wave] = any_w;
-  double* const mine = lds.red[wave & 3] + lane;
-  if (wave >= 4) {
+  // Sums over the wavefronts in their order.  Element v of a lane is token (v & 3) + 8 (v >> 2) + 4 g of the lane's expert.
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      mine[64 * v] = even[v];
-      mine[64 * (16 + v)] = odd[v];
+  for (int i = 0; i < 4; ++i) {   // over the eight lanes of a token
+    float n = nx[i];
+    int o = static_cast<int>(orx[i] & 0x7FFF7FFFu);
+    n += dpp<0xB1>(n); n += dpp<0x4E>(n); n += dpp<0x141>(n);
+    o |= dpp<0xB1>(o); o |= dpp<0x4E>(o); o |= dpp<0x141>(o);
+    if ((lane & 7) == 0) {
+      lds.nx[wave][8 * i + (lane >> 3)] = n;
+      lds.orx[wave][8 * i + (lane >> 3)] = o;
     }
   }
-  __syncthreads();
-  if (wave < 4) {
+  if constexpr (!LAID) {
+    lds.nw[wave][2 * r + 64 * g] = nw[0];
+    lds.nw[wave][2 * r + 64 * g + 1] = nw[1];
+    const bool any_w = __ballot((orw & 0x7FFF7FFFu) != 0) != 0;
+    if (lane == 0) lds.orw[wave] = any_w;
+  } else {
+    lds.nw[wave][lane] = op_n;
+    op_any = __ballot(op_any != 0) != 0;
+    if (lane == 0) lds.orw[wave] = op_any;
+  }
+  __syncthreads();   // the sums take the place of the rows
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      mine[64 * v] += even[v];
-      mine[64 * (16 + v)] += odd[v];
+  for (int f = 0; f < NF; ++f)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) lds.red[wave][64 * (16 * f + v) + lane] = acc[f][v];
+  if (wave == 0) {
+    // |w|^2 of expert `lane`; a bound that is not a number must not get lost in the maximum
+    float n = 0.0f;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < kRtWaves; ++i) {
+      n += LAID ? lds.nw[i][lane] : lds.nw[i][lane] + lds.nw[i][lane + 64];
+      any |= lds.orw[i];
     }
+    n = lane < a.E ? (n == n ? n : INFINITY) : 0.0f;
+    n = row_max(n);
+    n = fmaxf(n, __shfl_xor(n, 16, 64));
+    n = fmaxf(n, __shfl_xor(n, 32, 64));
+    if (lane == 0) lds.w2 = any ? fmaxf(n, 0x1p-149f) : 0.0f;
+  } else if (wave == 1 && lane < kRtTokens) {
+    float n = 0.0f;
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < kRtWaves; ++i) {
+      n += lds.nx[i][lane];
+      any |= lds.orx[i][lane];
+    }
+    lds.x2[lane] = any ? fmaxf(n == n ? n : INFINITY, 0x1p-149f) : 0.0f;   // zero only for zeros
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2 * NF; ++i) {
     const int at = tid + i * kRtThreads;
-    const double sum = ((lds.red[0][at] + lds.red[1][at]) + lds.red[2][at]) + lds.red[3][at];
+    double sum = lds.red[0][at];
+#pragma unroll
+    for (int w = 1; w < kRtWaves; ++w) sum += lds.red[w][at];
     const int v = at >> 6, ln = at & 63;
-    lds.l[(v & 3) + 8 * ((v >> 2) & 3) + 4 * (ln >> 5)][2 * (ln & 31) + (v >> 4)] = sum;
+    lds.l[(v & 3) + 8 * ((v >> 2) & 3) + 4 * (ln >> 5)][NF == 2 ? 2 * (ln & 31) + (v >> 4) : ln & 31] = sum;
   }
+  if (tid == 0) lds.n_pairs = 0;
   __syncthreads();
 
   // Selection: 16 lanes per token, all 32 at once.
   const int t = tid >> 4, s = tid & 15, tok = t0 + t;
   const bool live = tok < a.T;
   const bool masked = live && a.mask != nullptr && a.mask[tok] == 0;
-  float x2 = lds.nx[s & 7][t + 32 * (s >> 3)];
-  int bits = static_cast<int>(lds.orx[s & 7][t + 32 * (s >> 3)]);
-  x2 = row_sum(x2);
-  bits = row_or(bits);
-  float w2 = 0.0f;
-  int w_nan = 0;
-  uint32_t wbits = 0;
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {   // lane s: experts s + 16 v
-    float n = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kRtWaves; ++i) n += lds.nw[i][s & 1][(s >> 1) + 8 * v] + lds.nw[i][s & 1][(s >> 1) + 8 * v + 32];
-    const bool in = s + 16 * v < a.E;
-    w2 = fmaxf(w2, in ? n : 0.0f);
-    w_nan |= in && n != n;
-  }
-#pragma unroll
-  for (int i = 0; i < kRtWaves; ++i) wbits |= lds.orw[i];
-  w_nan = row_or(w_nan);
-  w2 = row_max(w2);
   // squares that underflow say nothing; products below the smallest normal value are off by an absolute amount
-  const bool zero = bits == 0 || wbits == 0;
+  const float x2 = lds.x2[t], w2 = lds.w2;
+  const bool zero = x2 == 0.0f || w2 == 0.0f;   // all logits are exactly zero
   float tol = kRtBound * sqrtf(x2) * sqrtf(w2) + 0x1p-120f;
-  if (w_nan || !(x2 > 0x1p-80f && w2 > 0x1p-80f)) tol = INFINITY;
+  if (!(x2 > 0x1p-80f && w2 > 0x1p-80f)) tol = INFINITY;
   if (zero) tol = 0.0f;
-  float sc[4], shift, total;
-  float* const fkey = reinterpret_cast<float*>(lds.pick.key[t]);
-  float* const fgrp = reinterpret_cast<float*>(lds.pick.grp[t]);
   const bool vague = !(tol < INFINITY);   // the bound says nothing: every logit of the token is settled
-  const bool close = (route_select<float>(a, lds.l[t], fkey, fgrp, lds.sel[t], tol, 0, nullptr, sc, shift, total) || vague) && live && !masked;
-  if (__ballot(close)) {   // rare: settle what is too close
-    int exact = zero ? 15 : 0, again = 0, all = 0;
+  float sc[4], total;
+  double shift;
+  route_scores(a, lds.l[t], sc, shift, total);
+  int again = route_select(a, lds.l[t], sc, shift, reinterpret_cast<int*>(lds.pick.key[t]), reinterpret_cast<int*>(lds.pick.grp[t]), lds.pick.m[t],
+                           lds.sel[t], tol);
+  if (vague) {
+    again = 16;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) all |= s + 16 * v < a.E ? 1 << v : 0;
-    for (;;) {
-      if (s < 8) lds.sel[t][s] = -1;
-      wave_lds_fence();
-      route_select<double>(a, lds.l[t], lds.pick.key[t], lds.pick.grp[t], lds.sel[t], tol, exact, &again, sc, shift, total);
-      again = close ? (vague ? all : again) & ~exact : 0;
-      uint64_t b[4];
+    for (int v = 0; v < 4; ++v) again |= s + 16 * v < a.E ? 1 << v : 0;
+  }
+  if (!live || masked) again = 0;
+  // Rare: the logits that a selection hangs on are settled, and it is made again in fp64, until it hangs on none.
+  uint64_t b[5];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) b[v] = __ballot(again >> v & 1);
-      if (!(b[0] | b[1] | b[2] | b[3])) break;
-      for (int q = 0; q < 4; ++q) {
-        uint64_t m = 0;
+  for (int v = 0; v < 5; ++v) b[v] = __ballot(again >> v & 1);
+  const bool redo = (b[0] | b[1] | b[2] | b[3]) != 0;
+  if (__syncthreads_or(redo)) {
+    const uint64_t all = ~0ull >> (64 - a.E);
+    uint64_t exact[4];
+    const bool pairs_do = a.sigmoid || keys_are_logits(a);
+    int todo = 0, two = 0;   // tokens of this wavefront; those with two experts to put in order
 #pragma unroll
-        for (int v = 0; v < 4; ++v) m |= ((b[v] >> (16 * q)) & 0xFFFFull) << (16 * v);
-        while (m) {
-          const int e0 = __builtin_ctzll(m);
-          m &= m - 1;
-          const int e1 = m ? __builtin_ctzll(m) : e0;
-          if (m) m &= m - 1;
-          exact_logits(a, t0 + (wave << 2) + q, e0, e1, lds.l[(wave << 2) + q]);
-        }
-      }
-      exact |= again;
-      wave_lds_fence();
+    for (int q = 0; q < 4; ++q) {
+      uint64_t m = 0;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) m |= ((b[v] >> (16 * q)) & 0xFFFFull) << (16 * v);
+      todo |= m ? 1 << q : 0;
+      if (pairs_do && __builtin_popcountll(m) == 2 && !((b[4] >> (16 * q)) & 0xFFFF) && !__builtin_amdgcn_readlane(zero, 16 * q)) two |= 1 << q;
+      exact[q] = __builtin_amdgcn_readlane(zero, 16 * q) ? all : m;
+      if (exact[q] == m && (m >> lane & 1)) lds.pick.pairs[atomicAdd(&lds.n_pairs, 1)] = (4 * wave + q) << 6 | lane;
     }
+    for (;;) {
+      if (!__syncthreads_or(todo)) break;
+      settle_logits<LAID>(a, t0, lds);
+      __syncthreads();
+      if (tid == 0) lds.n_pairs = 0;
+      __syncthreads();
+#pragma unroll 1
+      for (int q = 0; q < 4; ++q) {
+        if (!(todo >> q & 1)) continue;
+        const int tq = 4 * wave + q;
+        const float tol_q = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(tol), 16 * q));
+        const uint64_t done = q == 0 ? exact[0] : q == 1 ? exact[1] : q == 2 ? exact[2] : exact[3];
+        if (two >> q & 1) {
+          order_two(a, lds.l[tq], lds.sel[tq], __builtin_ctzll(done), 63 - __builtin_clzll(done));
+          todo &= ~(1 << q);
+          continue;
+        }
+        const uint64_t next = route_select_exact(a, lds.l[tq], lds.pick.key[tq], lds.pick.grp[tq], lds.sel[tq], tol_q, done);
+        if (next == 0) todo &= ~(1 << q);
+        if (next >> lane & 1) lds.pick.pairs[atomicAdd(&lds.n_pairs, 1)] = tq << 6 | lane;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i == q) exact[i] |= next;
+      }
+    }
+    if (redo) route_scores(a, lds.l[t], sc, shift, total);
   }
   wave_lds_fence();
   // weights: lane j < k has slot j
-  const int e = s < a.k && !masked ? static_cast<volatile int*>(lds.sel[t])[s] : -1;
+  const int e = s < a.k && !masked ? lds.sel[t][s] : -1;
   const bool have = e >= 0;
   const double l = have ? lds.l[t][e] : 0.0;
   float w = 0.0f;
   if (a.renormalise) {
     // a softmax over log s of the selected (softmax scores: log s is the logit up to a constant of the row)
-    const float ref = row_max(have ? static_cast<float>(l) : -INFINITY);
-    float al = static_cast<float>(l - static_cast<double>(ref));
+    float al = static_cast<float>(l - row_max(have ? l : static_cast<double>(-INFINITY)));
     if (a.sigmoid) {
       const float lf = static_cast<float>(l);
-      al = fminf(lf, 0.0f) - log1pf(expf(-fabsf(lf)));
-      const float top = row_max(have ? al : -INFINITY);
-      al -= top;
+      al = fminf(lf, 0.0f) - 0.69314718f * __builtin_amdgcn_logf(1.0f + exp_of(-fabsf(lf)));
+      al -= row_max(have ? al : -INFINITY);
     }
-    const float ex = have ? expf(al) : 0.0f;
+    const float ex = have ? exp_of(al) : 0.0f;
     w = ex / row_sum(ex);
   } else {
-    w = a.sigmoid ? 1.0f / (1.0f + expf(-static_cast<float>(l))) : expf(static_cast<float>(l - static_cast<double>(shift))) / total;
+    w = a.sigmoid ? 1.0f / (1.0f + exp_of(-static_cast<float>(l))) : exp_of(static_cast<float>(l - shift)) / total;
   }
   if (live && s < a.k) {
     a.topk_idx[static_cast<int64_t>(tok) * a.k + s] = e;
@@ -488,56 +755,92 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
     double d = live && !masked ? static_cast<double>(sc[v]) : 0.0;
     d += __shfl_xor(d, 16, 64);
     d += __shfl_xor(d, 32, 64);
-    if (lane < 16) lds.sum[wave][lane + 16 * v] = d;
+    if (lane < 16) lds.pick.sum[wave][lane + 16 * v] = d;
   }
   __syncthreads();
   if (tid < 64) {
     double d = 0.0;
 #pragma unroll
-    for (int i = 0; i < kRtWaves; ++i) d += lds.sum[i][tid];
+    for (int i = 0; i < kRtWaves; ++i) d += lds.pick.sum[i][tid];
     a.part_sum[static_cast<int64_t>(blockIdx.x) * 64 + tid] = d;
     a.part_cnt[static_cast<int64_t>(blockIdx.x) * 64 + tid] = lds.cnt[tid];
   }
 }
 
-// Counts and score sums of all workgroups, in their order.
+// Counts and score sums of all workgroups in a fixed order: 16 experts per workgroup, 64 slices of the partial sums.
 __global__ __launch_bounds__(1024) void route_stats_kernel(const double* __restrict__ part_sum, const int32_t* __restrict__ part_cnt, int blocks,
                                                            int E, int32_t* __restrict__ counts, float* __restrict__ score_sum) {
-  __shared__ double s_sum[16][64];
-  __shared__ int s_cnt[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ double s_sum[64][17];
+  __shared__ int s_cnt[64][17];
+  const int col = threadIdx.x & 15, slice = threadIdx.x >> 4, e = blockIdx.x * 16 + col;
   double a = 0.0;
   int c = 0;
-  for (int b = wave; b < blocks; b += 16) {
-    if (score_sum != nullptr) a += part_sum[static_cast<int64_t>(b) * 64 + lane];
-    if (counts != nullptr) c += part_cnt[static_cast<int64_t>(b) * 64 + lane];
+#pragma unroll 8
+  for (int b = slice; b < blocks; b += 64) {
+    a += part_sum[static_cast<int64_t>(b) * 64 + e];
+    c += part_cnt[static_cast<int64_t>(b) * 64 + e];
   }
-  s_sum[wave][lane] = a;
-  s_cnt[wave][lane] = c;
+  s_sum[slice][col] = a;
+  s_cnt[slice][col] = c;
   __syncthreads();
-  if (wave == 0 && lane < E) {
-    for (int w = 1; w < 16; ++w) { a += s_sum[w][lane]; c += s_cnt[w][lane]; }
-    if (score_sum != nullptr) score_sum[lane] = static_cast<float>(a);
-    if (counts != nullptr) counts[lane] = c;
+  if (threadIdx.x < 256) {   // 16 lanes per expert, four slices each
+    const int i = threadIdx.x >> 4, q = threadIdx.x & 15;
+    a = (s_sum[q][i] + s_sum[q + 16][i]) + (s_sum[q + 32][i] + s_sum[q + 48][i]);
+    c = (s_cnt[q][i] + s_cnt[q + 16][i]) + (s_cnt[q + 32][i] + s_cnt[q + 48][i]);
+    a = row_sum(a);
+    c = row_sum(c);
+    const int expert = blockIdx.x * 16 + i;
+    if (q == 0 && expert < E) {
+      if (score_sum != nullptr) score_sum[expert] = static_cast<float>(a);
+      if (counts != nullptr) counts[expert] = c;
+    }
   }
 }
 
 static int route_blocks(int T) { return (T + kRtTokens - 1) / kRtTokens; }
+static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
+static int route_operands(int E) { return E <= 32 ? 1 : 2; }
 
-size_t route_workspace_bytes(int T) { return 256 + static_cast<size_t>(route_blocks(T)) * 64 * (sizeof(double) + sizeof(int32_t)); }
+size_t route_workspace_bytes(int T, int d, int E, bool stats) {
+  size_t n = 0;
+  if (stats) n += align256(static_cast<size_t>(route_blocks(T)) * 64 * (sizeof(double) + sizeof(int32_t)) + 1);
+  if (T > kRouteFewTokens) n += align256(static_cast<size_t>(d / kRtUnit) * (4 * route_operands(E) * 1024 + 64 * 8) + static_cast<size_t>(E) * d * 2);
+  return n;
+}
 
 hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, hipStream_t stream) {
-  const int blocks = route_blocks(a.T);
+  const int blocks = route_blocks(a.T), units = a.d / kRtUnit;
   const bool stats = counts != nullptr || score_sum != nullptr;
+  char* ws = static_cast<char*>(workspace);
   if (stats) {
-    a.part_sum = static_cast<double*>(workspace);
+    a.part_sum = reinterpret_cast<double*>(ws);
     a.part_cnt = reinterpret_cast<int32_t*>(a.part_sum + static_cast<int64_t>(blocks) * 64);
+    ws += align256(static_cast<size_t>(blocks) * 64 * (sizeof(double) + sizeof(int32_t)) + 1);
   }
-  if (a.T > 0) {
-    if (a.E % 2 == 0 && (reinterpret_cast<uintptr_t>(a.w_router) & 3) == 0) route_kernel<true><<<blocks, kRtThreads, 0, stream>>>(a);
-    else route_kernel<false><<<blocks, kRtThreads, 0, stream>>>(a);
+  if (a.T > kRouteFewTokens) {
+    const int nf = route_operands(a.E);
+    u4* const ops = reinterpret_cast<u4*>(ws);
+    u4* const cols = ops + static_cast<int64_t>(units) * 4 * nf * 64;
+    float* const w2 = reinterpret_cast<float*>(cols + static_cast<int64_t>(a.E) * a.d / 8);
+    uint32_t* const bits = reinterpret_cast<uint32_t*>(w2 + units * 64);
+    a.ops = ops;
+    a.cols = cols;
+    a.op_w2 = w2;
+    a.op_bits = bits;
+    if (nf == 1) {
+      route_layout_kernel<1><<<units, 256, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
+      route_kernel<1, true, 4, true><<<blocks, kRtThreads, 0, stream>>>(a);
+    } else {
+      route_layout_kernel<2><<<units, 256, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
+      route_kernel<2, true, 8, true><<<blocks, kRtThreads, 0, stream>>>(a);
+    }
+  } else if (a.T > 0) {
+    if (a.E <= 16 && a.E % 2 == 0) route_kernel<2, false, 2, true><<<blocks, kRtThreads, 0, stream>>>(a);
+    else if (a.E <= 16) route_kernel<2, false, 2, false><<<blocks, kRtThreads, 0, stream>>>(a);
+    else if (a.E % 2 == 0) route_kernel<2, false, 8, true><<<blocks, kRtThreads, 0, stream>>>(a);
+    else route_kernel<2, false, 8, false><<<blocks, kRtThreads, 0, stream>>>(a);
   }
-  if (stats) route_stats_kernel<<<1, 1024, 0, stream>>>(a.part_sum, a.part_cnt, blocks, a.E, counts, score_sum);
+  if (stats) route_stats_kernel<<<(a.E + 15) / 16, 1024, 0, stream>>>(a.part_sum, a.part_cnt, blocks, a.E, counts, score_sum);
   return hipGetLastError();
 }
 

@@ -131,8 +131,9 @@ def test_route_refuses_on_the_host(lib):
         assert call(**bad) == 2, bad
     assert call(counts=P, ws_bytes=64) == 3
     assert call(T=0, x=None, w=None, idx=None, wt=None) == 0          # nothing to do
-    assert lib.mote_route_workspace_bytes(-1, 8) == 0 and lib.mote_route_workspace_bytes(4, 65) == 0
-    assert lib.mote_route_workspace_bytes(0, 8) > 0
+    assert lib.mote_route_workspace_bytes(-1, 256, 8) == 0 and lib.mote_route_workspace_bytes(4, 256, 65) == 0
+    assert lib.mote_route_workspace_bytes(4, 100, 8) == 0 and lib.mote_route_workspace_bytes(0, 256, 8) > 0
+    assert call(T=65, ws=None) == 1 and call(T=65, ws_bytes=1024) == 3     # the laid out weights
 
 
 def test_route_backward_refuses_on_the_host(lib):
