@@ -238,7 +238,11 @@ struct RouteBackwardArgs {
   float scale;
   float* dx;                  // or null
   float* dw;                  // or null
-  float* g;                   // [T, 64] dL/dlogits
+  // workspace: dlogits as operands of both products, the weights as operands of dx, shares of dw
+  unsigned int __attribute__((ext_vector_type(4)))* ga;
+  unsigned int __attribute__((ext_vector_type(4)))* gb;
+  unsigned int __attribute__((ext_vector_type(4)))* wa;
+  float* dw_part;
 };
 size_t route_backward_workspace_bytes(int T, int d, int E);
 hipError_t launch_route_backward(RouteBackwardArgs a, void* workspace, hipStream_t stream);

@@ -958,45 +958,324 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
     if (!live || masked || s + 16 * v >= E) g[v] = 0.0f;
 }
 
-__global__ __launch_bounds__(256) void route_dlogits_kernel(RouteBackwardArgs a) {
-  const int tok = blockIdx.x * 16 + (threadIdx.x >> 4), s = threadIdx.x & 15;
+// The two products of the gradient run on the bf16 MFMA with exact operands: x and w_router are bf16, an fp32 dlogits is the sum of
+// three bf16 terms (8 bits of its 24 each, cut and not rounded, so that the rest is exact).  route_dlogits_kernel writes the
+// terms as operands of both:
+//   ga [tile of 32 tokens][term][step of 16 experts][lane]: lane 32 g + r, experts 16 s + 8 g .. + 7 of token r        (dx)
+//   gb [step of 16 tokens][term][32 experts][lane]: lane 32 g + r, tokens 8 g .. + 7 of the step, expert 32 n + r      (dw)
+// and the router's weights for dx, wa [32 channels][step of 16 experts][lane]: experts 16 s + 8 g .. + 7 of channel r.
+// Bound of the whole: HBM, x read once and dx (fp32) written once; the terms are 12 bytes per token and expert and stay in the caches.
+__device__ __forceinline__ void three_terms(float g, uint32_t (&t)[3]) {
+  const uint32_t b = __float_as_uint(g);
+  if ((b & 0x7F800000u) == 0x7F800000u) {   // infinity and NaN: one term
+    t[0] = (b >> 16) | ((b & 0x7FFFFFu) ? 0x40u : 0u);
+    t[1] = t[2] = 0u;
+    return;
+  }
+  const float r1 = g - __uint_as_float(b & 0xFFFF0000u);
+  const uint32_t b1 = __float_as_uint(r1);
+  const float r2 = r1 - __uint_as_float(b1 & 0xFFFF0000u);
+  t[0] = b >> 16;
+  t[1] = b1 >> 16;
+  t[2] = __float_as_uint(r2) >> 16;
+}
+
+// 32 tokens per workgroup, 16 lanes each; the workgroups behind those lay out the weights, 32 channels each.
+// NS: steps of 16 experts, NT: tiles of 32.
+template <int NS, int NT>
+__global__ __launch_bounds__(512) void route_dlogits_kernel(RouteBackwardArgs a) {
+  __shared__ float s_g[32][65];
+  const int tid = threadIdx.x, tiles = (a.T + 31) / 32;
+  if (static_cast<int>(blockIdx.x) >= tiles) {
+    const int ct = blockIdx.x - tiles;
+    for (int i = tid; i < NS * 64; i += 512) {
+      const int lane = i & 63, s = i >> 6, e = 16 * s + 8 * (lane >> 5);
+      const uint16_t* const row = a.w_router + static_cast<int64_t>(32 * ct + (lane & 31)) * a.E;
+      u4 o;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t lo = e + 2 * q < a.E ? row[e + 2 * q] : 0, hi = e + 2 * q + 1 < a.E ? row[e + 2 * q + 1] : 0;
+        o[q] = lo | hi << 16;
+      }
+      a.wa[static_cast<int64_t>(ct) * NS * 64 + i] = o;
+    }
+    return;
+  }
+  const int t = tid >> 4, s = tid & 15, tok = blockIdx.x * 32 + t;
   float g[4];
   route_grad_token(a, min(tok, a.T - 1), tok < a.T, g);
-  if (tok < a.T)
 #pragma unroll
-    for (int v = 0; v < 4; ++v) a.g[static_cast<int64_t>(tok) * 64 + s + 16 * v] = g[v];
-}
-
-__global__ __launch_bounds__(256) void route_dx_kernel(RouteBackwardArgs a) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= static_cast<int64_t>(a.T) * a.d) return;
-  const int64_t t = i / a.d;
-  const int c = static_cast<int>(i - t * a.d);
-  float s = 0.0f;
-  for (int e = 0; e < a.E; ++e) s = fmaf(a.g[t * 64 + e], bf16_to_f32(a.w_router[static_cast<int64_t>(c) * a.E + e]), s);
-  a.dx[i] = s;
-}
-
-__global__ __launch_bounds__(256) void route_dw_kernel(RouteBackwardArgs a) {
-  const int c = blockIdx.x, e = threadIdx.x & 63, part = threadIdx.x >> 6;
-  __shared__ float s_p[4][64];
-  float s = 0.0f;
-  for (int t = part; t < a.T; t += 4) s = fmaf(bf16_to_f32(a.x[static_cast<int64_t>(t) * a.d + c]), a.g[static_cast<int64_t>(t) * 64 + e], s);
-  s_p[part][e] = s;
+  for (int v = 0; v < 4; ++v) s_g[t][s + 16 * v] = g[v];
   __syncthreads();
-  if (threadIdx.x < a.E) a.dw[static_cast<int64_t>(c) * a.E + e] = ((s_p[0][e] + s_p[1][e]) + s_p[2][e]) + s_p[3][e];
+#pragma unroll 1
+  for (int i = tid; i < (NS + 2 * NT) * 64; i += 512) {
+    const bool first = i < NS * 64;
+    const int j = first ? i : i - NS * 64, lane = j & 63, q = j >> 6;      // q: step of experts, or 2 * tile of experts + step of tokens
+    const int at_t = first ? lane & 31 : 16 * (q & 1) + 8 * (lane >> 5), at_e = first ? 16 * q + 8 * (lane >> 5) : 32 * (q >> 1) + (lane & 31);
+    u4 o[3];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      uint32_t lo[3], hi[3];
+      three_terms(first ? s_g[at_t][at_e + 2 * h] : s_g[at_t + 2 * h][at_e], lo);
+      three_terms(first ? s_g[at_t][at_e + 2 * h + 1] : s_g[at_t + 2 * h + 1][at_e], hi);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) o[p][h] = lo[p] | hi[p] << 16;
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      if (first) a.ga[((static_cast<int64_t>(blockIdx.x) * 3 + p) * NS + q) * 64 + lane] = o[p];
+      else a.gb[((static_cast<int64_t>(blockIdx.x) * 2 + (q & 1)) * 3 + p) * (NT * 64) + (q >> 1) * 64 + lane] = o[p];
+    }
+  }
 }
 
-size_t route_backward_workspace_bytes(int T, int d, int E) {
-  (void)d; (void)E;
-  return 256 + static_cast<size_t>(T) * 64 * sizeof(float);
+__device__ __forceinline__ v16f mfma_bf16(u4 a, u4 b, v16f c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
+
+// dx: a wavefront has 64 tokens, whose terms stay in registers, and 256 channels, whose weights come 32 channels at a time.
+constexpr int kDxChannels = 256;
+template <int NS>
+__global__ __launch_bounds__(256) void route_dx_kernel(RouteBackwardArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, g = lane >> 5;
+  const int c_begin = (blockIdx.y * 4 + wave) * kDxChannels, c_end = min(c_begin + kDxChannels, a.d);
+  if (c_begin >= a.d) return;
+  const int tile = blockIdx.x * 2, tiles = (a.T + 31) / 32;
+  u4 ga[2][3][NS];
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) ga[m][p][s] = a.ga[((static_cast<int64_t>(min(tile + m, tiles - 1)) * 3 + p) * NS + s) * 64 + lane];
+  u4 w[NS];
+  auto load = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) w[s] = a.wa[(static_cast<int64_t>(min(c, a.d - 32) >> 5) * NS + s) * 64 + lane];
+  };
+  load(c_begin);
+#pragma unroll 1
+  for (int c = c_begin; c < c_end; c += 32) {
+    v16f acc[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[m][v] = 0.0f;
+    u4 b[NS];
+#pragma unroll
+    for (int s = 0; s < NS; ++s) b[s] = w[s];
+    load(c + 32);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int p = 2; p >= 0; --p)   // smallest terms first
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) acc[m] = mfma_bf16(ga[m][p][s], b[s], acc[m]);
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int t = (tile + m) * 32 + (v & 3) + 8 * (v >> 2) + 4 * g;
+        if (t < a.T) a.dx[static_cast<int64_t>(t) * a.d + c + r] = acc[m][v];
+      }
+  }
+}
+
+// dw: a workgroup has 128 channels and a share of the tokens, which its eight wavefronts split; their sums meet in LDS.  A
+// step is 16 tokens: 4 KB of x as it lies in memory, turned into operands through LDS (a word of two channels of eight
+// tokens each: even and odd channels are two operands), against the terms of the step.  With several shares
+// (blockIdx.y) the sums go to dw_part, which route_dw_sum_kernel adds in order.
+constexpr int kDwWaves = 8, kDwChannels = 128;
+template <int NT>
+__global__ __launch_bounds__(64 * kDwWaves) void route_dw_kernel(RouteBackwardArgs a, int steps_per_wave) {
+  __shared__ __attribute__((aligned(16))) union {
+    unsigned char x[kDwWaves][16 * 2 * kDwChannels];
+    float sum[kDwWaves / 2][4 * NT * 16][64];
+  } lds;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, g = lane >> 5;
+  const int c0 = blockIdx.x * kDwChannels, steps = (a.T + 15) / 16;
+  const int first = (blockIdx.y * kDwWaves + wave) * steps_per_wave, last = min(first + steps_per_wave, steps);
+  v16f acc[2][2][NT];   // half of the channels, even / odd, tile of experts
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[j][o][n][v] = 0.0f;
+  struct Step {
+    u4 x[4], g[3][NT];
+  };
+  auto load = [&](int s) __attribute__((always_inline)) {
+    Step q;
+    s = min(s, last - 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = 16 * s + 4 * i + (lane >> 4);
+      const uint16_t* const row = a.x + static_cast<int64_t>(min(t, a.T - 1)) * a.d + c0 + 8 * (lane & 15);
+      q.x[i] = *reinterpret_cast<const u4*>(row);
+      // a padding token has no part, whatever its row holds
+      const bool out = t >= a.T || (a.mask != nullptr && a.mask[min(t, a.T - 1)] == 0);
+      if (out) q.x[i] = u4{0u, 0u, 0u, 0u};
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) q.g[p][n] = a.gb[(static_cast<int64_t>(s) * 3 + p) * (NT * 64) + n * 64 + lane];
+    __builtin_amdgcn_sched_barrier(0);
+    return q;
+  };
+  unsigned char* const stage = lds.x[wave];
+  auto compute = [&](const Step& q) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u4*>(stage + 1024 * i + 16 * lane) = q.x[i];
+    wave_lds_fence();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const uint32_t*>(stage + (8 * g + i) * 256 + 128 * j + 4 * r);
+      u4 even, odd;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        even[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
+        odd[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+      }
+#pragma unroll
+      for (int p = 2; p >= 0; --p)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          acc[j][0][n] = mfma_bf16(even, q.g[p][n], acc[j][0][n]);
+          acc[j][1][n] = mfma_bf16(odd, q.g[p][n], acc[j][1][n]);
+        }
+    }
+    wave_lds_fence();
+  };
+  if (first < last) {
+    Step p = load(first), q;
+#pragma unroll 1
+    for (int s = first; s < last; s += 2) {
+      q = load(s + 1);
+      compute(p);
+      if (s + 1 >= last) break;
+      p = load(s + 2);
+      compute(q);
+    }
+  }
+  // sums of the wavefronts, a tree in a fixed order
+#pragma unroll 1
+  for (int half = kDwWaves / 2; half > 0; half >>= 1) {
+    __syncthreads();
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) lds.sum[wave - half][((j * 2 + o) * NT + n) * 16 + v][lane] = acc[j][o][n][v];
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int o = 0; o < 2; ++o)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[j][o][n][v] += lds.sum[wave][((j * 2 + o) * NT + n) * 16 + v][lane];
+    }
+  }
+  if (wave != 0) return;
+  const bool whole = gridDim.y == 1;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int c = c0 + 64 * j + 2 * ((v & 3) + 8 * (v >> 2) + 4 * g) + o, e = 32 * n + r;
+          if (!whole) a.dw_part[(static_cast<int64_t>(blockIdx.y) * a.d + c) * (32 * NT) + e] = acc[j][o][n][v];
+          else if (e < a.E) a.dw[static_cast<int64_t>(c) * a.E + e] = acc[j][o][n][v];
+        }
+}
+
+template <int NT>
+__global__ __launch_bounds__(256) void route_dw_sum_kernel(const float* __restrict__ part, int parts, int d, int E, float* __restrict__ dw) {
+  const int i = blockIdx.x * 256 + threadIdx.x, c = i / (32 * NT), e = i % (32 * NT);
+  if (c >= d) return;
+  const int64_t stride = static_cast<int64_t>(d) * 32 * NT;
+  float s = 0.0f;
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) s += part[p * stride + i];
+  if (e < E) dw[static_cast<int64_t>(c) * E + e] = s;
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(float* __restrict__ p, int64_t n) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i < n) p[i] = 0.0f;
+}
+
+namespace {
+int steps_of(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : 4; }
+// Shares of the tokens: enough workgroups for every CU, at least eight steps of 16 tokens for each wavefront while there are that many
+int dw_shares(int T, int d) {
+  const int want = std::max(256 / (d / kDwChannels), 1), most = (T + 16 * kDwWaves * 8 - 1) / (16 * kDwWaves * 8);
+  return std::max(std::min(want, most), 1);
+}
+struct BackwardLayout {
+  size_t ga, gb, wa, part, bytes;
+};
+BackwardLayout backward_layout(int T, int d, int E) {
+  const size_t tiles = (static_cast<size_t>(T) + 31) / 32, ns = steps_of(E), nt = E <= 32 ? 1 : 2;
+  BackwardLayout l;
+  size_t at = 0;
+  auto take = [&](size_t n) { const size_t p = at; at += align256(n); return p; };
+  l.ga = take(tiles * 3 * ns * 1024);
+  l.gb = take(tiles * 2 * 3 * nt * 1024);
+  l.wa = take(static_cast<size_t>(d / 32) * ns * 1024);
+  l.part = take(dw_shares(T, d) > 1 ? static_cast<size_t>(dw_shares(T, d)) * d * 32 * nt * sizeof(float) : 0);
+  l.bytes = std::max<size_t>(at, 256);
+  return l;
+}
+}  // namespace
+
+size_t route_backward_workspace_bytes(int T, int d, int E) { return backward_layout(T, d, E).bytes; }
 
 hipError_t launch_route_backward(RouteBackwardArgs a, void* workspace, hipStream_t stream) {
-  a.g = static_cast<float*>(workspace);
-  if (a.T > 0) route_dlogits_kernel<<<(a.T + 15) / 16, 256, 0, stream>>>(a);
-  if (a.T > 0 && a.dx) route_dx_kernel<<<static_cast<unsigned>((static_cast<int64_t>(a.T) * a.d + 255) / 256), 256, 0, stream>>>(a);
-  if (a.dw) route_dw_kernel<<<a.d, 256, 0, stream>>>(a);
+  if (a.T == 0) {
+    const int64_t n = static_cast<int64_t>(a.d) * a.E;
+    if (a.dw) zero_kernel<<<static_cast<unsigned>((n + 255) / 256), 256, 0, stream>>>(a.dw, n);
+    return hipGetLastError();
+  }
+  const BackwardLayout l = backward_layout(a.T, a.d, a.E);
+  char* const ws = static_cast<char*>(workspace);
+  a.ga = reinterpret_cast<u4*>(ws + l.ga);
+  a.gb = reinterpret_cast<u4*>(ws + l.gb);
+  a.wa = reinterpret_cast<u4*>(ws + l.wa);
+  a.dw_part = reinterpret_cast<float*>(ws + l.part);
+  const unsigned lay = static_cast<unsigned>((a.T + 31) / 32 + a.d / 32);
+  const dim3 dx_grid((a.T + 63) / 64, (a.d + 4 * kDxChannels - 1) / (4 * kDxChannels));
+  const int shares = dw_shares(a.T, a.d), steps = (a.T + 15) / 16, per_wave = (steps + shares * kDwWaves - 1) / (shares * kDwWaves);
+  const dim3 dw_grid(a.d / kDwChannels, shares);
+  const unsigned sum_grid = static_cast<unsigned>((static_cast<int64_t>(a.d) * (a.E <= 32 ? 32 : 64) + 255) / 256);
+#define MOTE_BACKWARD(NS_, NT_)                                                                                              \
+  route_dlogits_kernel<NS_, NT_><<<lay, 512, 0, stream>>>(a);                                                                \
+  if (a.dx) route_dx_kernel<NS_><<<dx_grid, 256, 0, stream>>>(a);                                                            \
+  if (a.dw) route_dw_kernel<NT_><<<dw_grid, 64 * kDwWaves, 0, stream>>>(a, per_wave);                                        \
+  if (a.dw && shares > 1) route_dw_sum_kernel<NT_><<<sum_grid, 256, 0, stream>>>(a.dw_part, shares, a.d, a.E, a.dw)
+  switch (steps_of(a.E)) {
+    case 1: MOTE_BACKWARD(1, 1); break;
+    case 2: MOTE_BACKWARD(2, 1); break;
+    default: MOTE_BACKWARD(4, 2); break;
+  }
+#undef MOTE_BACKWARD
   return hipGetLastError();
 }
 
