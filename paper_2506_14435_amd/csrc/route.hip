@@ -861,8 +861,8 @@ hipError_t launch_route_import(const int32_t* idx, const float* w, int n, int E,
 
 // -------------------------------------------------------------------------------------------------------- gradient
 
-// dL/dlogits of one token by 16 lanes (lane s: experts s + 16 v), fp32.
-__device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int tok, bool live, float (&g)[4]) {
+// dL/dlogits of one token by 16 lanes (lane s: experts s + 16 v), fp32.  slot_e, slot_d: LDS of the token's eight slots.
+__device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int tok, bool live, int* slot_e, float* slot_d, float (&g)[4]) {
   const int s = threadIdx.x & 15, E = a.E;
   float l[4], sc[4], om[4], up[4], sel[4], q[4];
   const int64_t row = static_cast<int64_t>(tok) * E;
@@ -876,14 +876,16 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
     sel[v] = 0.0f;
     mx = fmaxf(mx, l[v]);
   }
-  auto sum16 = [](float v) {
+  // every lane sees all slots: one load each, then LDS
+  if (s < 8) {
+    slot_e[s] = s < a.k ? a.topk_idx[static_cast<int64_t>(tok) * a.k + s] : -1;
+    slot_d[s] = s < a.k ? a.d_topk_w[static_cast<int64_t>(tok) * a.k + s] : 0.0f;
+  }
+  wave_lds_fence();
 #pragma unroll
-    for (int off = 8; off > 0; off >>= 1) v += __shfl_xor(v, off, 16);
-    return v;
-  };
-  for (int j = 0; j < a.k; ++j) {
-    const int e = a.topk_idx[static_cast<int64_t>(tok) * a.k + j];
-    const float d = a.d_topk_w[static_cast<int64_t>(tok) * a.k + j];
+  for (int j = 0; j < 8; ++j) {
+    const int e = slot_e[j];
+    const float d = slot_d[j];
 #pragma unroll
     for (int v = 0; v < 4; ++v)
       if (e == s + 16 * v && e < E) { up[v] += d; sel[v] += 1.0f; }
@@ -896,8 +898,7 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
       om[v] = l[v] >= 0.0f ? t * r : r;   // 1 - s
     }
   } else {
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 16));
+    mx = row_max(mx);
     float sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
@@ -905,7 +906,7 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
       om[v] = 1.0f;
       sum += sc[v];
     }
-    sum = sum16(sum);
+    sum = row_sum(sum);
 #pragma unroll
     for (int v = 0; v < 4; ++v) sc[v] /= sum;
   }
@@ -917,15 +918,14 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
       al[v] = a.sigmoid ? fminf(l[v], 0.0f) - log1pf(expf(-fabsf(l[v]))) : l[v];
       if (sel[v] > 0.0f) m = fmaxf(m, al[v]);
     }
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 16));
+    m = row_max(m);
     float p[4], sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       p[v] = sel[v] > 0.0f ? expf(al[v] - m) : 0.0f;
       sum += p[v] * sel[v];
     }
-    sum = sum16(sum);
+    sum = row_sum(sum);
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     float dot = 0.0f, dq = 0.0f;
 #pragma unroll
@@ -934,8 +934,8 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
       dot += p[v] * up[v];
       dq += sc[v] * q[v];
     }
-    dot = sum16(dot);
-    dq = sum16(dq);
+    dot = row_sum(dot);
+    dq = row_sum(dq);
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       g[v] = a.scale * p[v] * (up[v] - sel[v] * dot) * om[v];
@@ -948,7 +948,7 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
       up[v] = a.scale * up[v] + q[v];
       dot += sc[v] * up[v];
     }
-    dot = sum16(dot);
+    dot = row_sum(dot);
 #pragma unroll
     for (int v = 0; v < 4; ++v) g[v] = a.sigmoid ? sc[v] * om[v] * up[v] : sc[v] * (up[v] - dot);
   }
@@ -985,6 +985,8 @@ __device__ __forceinline__ void three_terms(float g, uint32_t (&t)[3]) {
 template <int NS, int NT>
 __global__ __launch_bounds__(512) void route_dlogits_kernel(RouteBackwardArgs a) {
   __shared__ float s_g[32][65];
+  __shared__ int s_e[32][8];
+  __shared__ float s_d[32][8];
   const int tid = threadIdx.x, tiles = (a.T + 31) / 32;
   if (static_cast<int>(blockIdx.x) >= tiles) {
     const int ct = blockIdx.x - tiles;
@@ -1003,7 +1005,7 @@ __global__ __launch_bounds__(512) void route_dlogits_kernel(RouteBackwardArgs a)
   }
   const int t = tid >> 4, s = tid & 15, tok = blockIdx.x * 32 + t;
   float g[4];
-  route_grad_token(a, min(tok, a.T - 1), tok < a.T, g);
+  route_grad_token(a, min(tok, a.T - 1), tok < a.T, s_e[t], s_d[t], g);
 #pragma unroll
   for (int v = 0; v < 4; ++v) s_g[t][s + 16 * v] = g[v];
   __syncthreads();
@@ -1033,12 +1035,12 @@ __device__ __forceinline__ v16f mfma_bf16(u4 a, u4 b, v16f c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// dx: a wavefront has 64 tokens, whose terms stay in registers, and 256 channels, whose weights come 32 channels at a time.
-constexpr int kDxChannels = 256;
+// dx: a wavefront has 64 tokens, whose terms stay in registers, and a slice of the channels, whose weights come 32 channels at
+// a time.  Slices of 256 channels (the terms are read once for 64 KB of dx), fewer while that leaves SIMDs without a wavefront.
 template <int NS>
-__global__ __launch_bounds__(256) void route_dx_kernel(RouteBackwardArgs a) {
+__global__ __launch_bounds__(256) void route_dx_kernel(RouteBackwardArgs a, int slice) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, g = lane >> 5;
-  const int c_begin = (blockIdx.y * 4 + wave) * kDxChannels, c_end = min(c_begin + kDxChannels, a.d);
+  const int c_begin = (blockIdx.y * 4 + wave) * slice, c_end = min(c_begin + slice, a.d);
   if (c_begin >= a.d) return;
   const int tile = blockIdx.x * 2, tiles = (a.T + 31) / 32;
   u4 ga[2][3][NS];
@@ -1107,6 +1109,8 @@ __global__ __launch_bounds__(64 * kDwWaves) void route_dw_kernel(RouteBackwardAr
         for (int v = 0; v < 16; ++v) acc[j][o][n][v] = 0.0f;
   struct Step {
     u4 x[4], g[3][NT];
+    uint32_t keep[4];   // 0: a padding token, which has no part whatever its row holds
+    int s;
   };
   auto load = [&](int s) __attribute__((always_inline)) {
     Step q;
@@ -1116,10 +1120,9 @@ __global__ __launch_bounds__(64 * kDwWaves) void route_dw_kernel(RouteBackwardAr
       const int t = 16 * s + 4 * i + (lane >> 4);
       const uint16_t* const row = a.x + static_cast<int64_t>(min(t, a.T - 1)) * a.d + c0 + 8 * (lane & 15);
       q.x[i] = *reinterpret_cast<const u4*>(row);
-      // a padding token has no part, whatever its row holds
-      const bool out = t >= a.T || (a.mask != nullptr && a.mask[min(t, a.T - 1)] == 0);
-      if (out) q.x[i] = u4{0u, 0u, 0u, 0u};
+      q.keep[i] = a.mask != nullptr ? a.mask[min(t, a.T - 1)] : 1u;
     }
+    q.s = s;
 #pragma unroll
     for (int p = 0; p < 3; ++p)
 #pragma unroll
@@ -1130,7 +1133,10 @@ __global__ __launch_bounds__(64 * kDwWaves) void route_dw_kernel(RouteBackwardAr
   unsigned char* const stage = lds.x[wave];
   auto compute = [&](const Step& q) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<u4*>(stage + 1024 * i + 16 * lane) = q.x[i];
+    for (int i = 0; i < 4; ++i) {
+      const bool in = q.keep[i] != 0 && 16 * q.s + 4 * i + (lane >> 4) < a.T;
+      *reinterpret_cast<u4*>(stage + 1024 * i + 16 * lane) = in ? q.x[i] : u4{0u, 0u, 0u, 0u};
+    }
     wave_lds_fence();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -1224,9 +1230,10 @@ __global__ __launch_bounds__(256) void zero_kernel(float* __restrict__ p, int64_
 
 namespace {
 int steps_of(int E) { return E <= 16 ? 1 : E <= 32 ? 2 : 4; }
-// Shares of the tokens: enough workgroups for every CU, at least eight steps of 16 tokens for each wavefront while there are that many
+// Shares of the tokens: one workgroup per CU, at least four steps of 16 tokens for each wavefront.  (d = 896, E = 8, T = 2048 with at
+// least eight: 12.8 us instead of 9.7; d = 2048, E = 64, T = 16000 with two workgroups per CU: 44.8 instead of 33.5.)
 int dw_shares(int T, int d) {
-  const int want = std::max(256 / (d / kDwChannels), 1), most = (T + 16 * kDwWaves * 8 - 1) / (16 * kDwWaves * 8);
+  const int want = std::max(256 / (d / kDwChannels), 1), most = (T + 16 * kDwWaves * 4 - 1) / (16 * kDwWaves * 4);
   return std::max(std::min(want, most), 1);
 }
 struct BackwardLayout {
@@ -1261,13 +1268,15 @@ hipError_t launch_route_backward(RouteBackwardArgs a, void* workspace, hipStream
   a.wa = reinterpret_cast<u4*>(ws + l.wa);
   a.dw_part = reinterpret_cast<float*>(ws + l.part);
   const unsigned lay = static_cast<unsigned>((a.T + 31) / 32 + a.d / 32);
-  const dim3 dx_grid((a.T + 63) / 64, (a.d + 4 * kDxChannels - 1) / (4 * kDxChannels));
+  int slice = 256;
+  while (slice > 32 && static_cast<int64_t>((a.T + 63) / 64) * ((a.d + slice - 1) / slice) < 1024) slice /= 2;
+  const dim3 dx_grid((a.T + 63) / 64, (a.d + 4 * slice - 1) / (4 * slice));
   const int shares = dw_shares(a.T, a.d), steps = (a.T + 15) / 16, per_wave = (steps + shares * kDwWaves - 1) / (shares * kDwWaves);
   const dim3 dw_grid(a.d / kDwChannels, shares);
   const unsigned sum_grid = static_cast<unsigned>((static_cast<int64_t>(a.d) * (a.E <= 32 ? 32 : 64) + 255) / 256);
 #define MOTE_BACKWARD(NS_, NT_)                                                                                              \
   route_dlogits_kernel<NS_, NT_><<<lay, 512, 0, stream>>>(a);                                                                \
-  if (a.dx) route_dx_kernel<NS_><<<dx_grid, 256, 0, stream>>>(a);                                                            \
+  if (a.dx) route_dx_kernel<NS_><<<dx_grid, 256, 0, stream>>>(a, slice);                                                      \
   if (a.dw) route_dw_kernel<NT_><<<dw_grid, 64 * kDwWaves, 0, stream>>>(a, per_wave);                                        \
   if (a.dw && shares > 1) route_dw_sum_kernel<NT_><<<sum_grid, 256, 0, stream>>>(a.dw_part, shares, a.d, a.E, a.dw)
   switch (steps_of(a.E)) {
