@@ -16,8 +16,8 @@ namespace {
 
 constexpr int kTable = 120;             // tensors of a launch: 3.8 KB of kernel arguments
 constexpr int kThreads = 256;
-constexpr int kChunk = 16384;           // elements of a unit of work
-constexpr int kMaxBlocks = 2048;        // workgroups of a launch
+constexpr int kUnit = 4096;             // elements of a unit of work: 64 (bf16: 32) bytes a thread, all on their way together
+constexpr int kSquareBlocks = 1024, kScaleBlocks = 2048;   // workgroups of a launch at most
 struct Table {
   const void* grad[kTable];
   void* out[kTable];
@@ -45,16 +45,61 @@ __device__ __forceinline__ double block_sum(double v, double* s) {
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
-template <typename T> __device__ __forceinline__ float to_f32(T v);
-template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_f32<uint16_t>(uint16_t v) { return bf16_to_f32(v); }
+// 16 bytes of a tensor
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ float get(const u4& v, int i) { return __uint_as_float(v[i]); }
+  static __device__ __forceinline__ u4 scaled(const u4& v, double c) {
+    u4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(static_cast<float>(get(v, i) * c));
+    return o;
+  }
+  static __device__ __forceinline__ float one(float v) { return v; }
+  static __device__ __forceinline__ float scaled_one(float v, double c) { return static_cast<float>(v * c); }
+};
+template <> struct Vec<uint16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ float get(const u4& v, int i) { return i & 1 ? bf16_hi(v[i >> 1]) : bf16_lo(v[i >> 1]); }
+  static __device__ __forceinline__ u4 scaled(const u4& v, double c) {
+    u4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = cvt_pk_bf16(static_cast<float>(bf16_lo(v[i]) * c), static_cast<float>(bf16_hi(v[i]) * c));
+    return o;
+  }
+  static __device__ __forceinline__ float one(uint16_t v) { return bf16_to_f32(v); }
+  static __device__ __forceinline__ uint16_t scaled_one(uint16_t v, double c) {
+    return static_cast<uint16_t>(cvt_pk_bf16(static_cast<float>(bf16_to_f32(v) * c), 0.0f));
+  }
+};
 
 template <typename T>
-__device__ __forceinline__ double square_unit(const T* g, int64_t n) {
+__device__ __forceinline__ double square_unit(const T* g, int n) {
+  constexpr int N = Vec<T>::N, V = kUnit / N / kThreads;
   double acc = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-    const double v = to_f32<T>(g[i]);
-    acc = fma(v, v, acc);
+  if (reinterpret_cast<uintptr_t>(g) % 16 == 0) {
+    const u4* const p = reinterpret_cast<const u4*>(g);
+    u4 v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (i * kThreads + static_cast<int>(threadIdx.x) + 1) * N <= n ? p[i * kThreads + threadIdx.x] : u4{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const double x = Vec<T>::get(v[i], j);
+        acc = fma(x, x, acc);
+      }
+    const int rest = n / N * N + threadIdx.x;
+    if (rest < n) {
+      const double x = Vec<T>::one(g[rest]);
+      acc = fma(x, x, acc);
+    }
+  } else {
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+      const double x = Vec<T>::one(g[i]);
+      acc = fma(x, x, acc);
+    }
   }
   return acc;
 }
@@ -62,9 +107,12 @@ __device__ __forceinline__ double square_unit(const T* g, int64_t n) {
 __global__ __launch_bounds__(kThreads) void grad_square_kernel(const Table t, double* __restrict__ partial) {
   __shared__ double s[4];
   double acc = 0.0;
-  for (int u = blockIdx.x; u < t.first[t.count]; u += gridDim.x) {
-    const int i = find(t, u);
-    const int64_t at = static_cast<int64_t>(u - t.first[i]) * kChunk, n = min(t.n[i] - at, static_cast<int64_t>(kChunk));
+  const int units = t.first[t.count];
+  int i = find(t, blockIdx.x);
+  for (int u = blockIdx.x; u < units; u += gridDim.x) {
+    while (t.first[i + 1] <= u) ++i;
+    const int64_t at = static_cast<int64_t>(u - t.first[i]) * kUnit;
+    const int n = static_cast<int>(min(t.n[i] - at, static_cast<int64_t>(kUnit)));
     acc += t.bf16[i >> 5] >> (i & 31) & 1 ? square_unit(static_cast<const uint16_t*>(t.grad[i]) + at, n)
                                           : square_unit(static_cast<const float*>(t.grad[i]) + at, n);
   }
@@ -72,29 +120,51 @@ __global__ __launch_bounds__(kThreads) void grad_square_kernel(const Table t, do
   if (threadIdx.x == 0) partial[blockIdx.x] = acc;
 }
 
+// c == 1: a copy, bits as they are
+template <typename T>
+__device__ __forceinline__ void scale_unit(const T* g, T* o, int n, bool clip, double c) {
+  constexpr int N = Vec<T>::N, V = kUnit / N / kThreads;
+  if ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(o)) % 16 == 0) {
+    const u4* const p = reinterpret_cast<const u4*>(g);
+    u4* const q = reinterpret_cast<u4*>(o);
+    u4 v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if ((i * kThreads + static_cast<int>(threadIdx.x) + 1) * N <= n) v[i] = p[i * kThreads + threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if ((i * kThreads + static_cast<int>(threadIdx.x) + 1) * N <= n) q[i * kThreads + threadIdx.x] = clip ? Vec<T>::scaled(v[i], c) : v[i];
+    const int rest = n / N * N + threadIdx.x;
+    if (rest < n) o[rest] = clip ? Vec<T>::scaled_one(g[rest], c) : g[rest];
+  } else {
+    for (int i = threadIdx.x; i < n; i += kThreads) o[i] = clip ? Vec<T>::scaled_one(g[i], c) : g[i];
+  }
+}
+
+// Units from the last to the first: what the kernel before read last is still in the memory-side cache.
 __global__ __launch_bounds__(kThreads) void grad_scale_kernel(const Table t, const double* __restrict__ partial, int partials, float max_norm,
                                                               float* __restrict__ norm_out) {
   __shared__ double s[4];
   double acc = 0.0;
+#pragma unroll 4
   for (int i = threadIdx.x; i < partials; i += kThreads) acc += partial[i];
   const double norm = sqrt(block_sum(acc, s));
   if (blockIdx.x == 0 && threadIdx.x == 0) norm_out[0] = static_cast<float>(norm);
   const double limit = max_norm;
   const bool clip = norm > limit && norm <= DBL_MAX;
   const double c = clip ? limit / norm : 1.0;   // fp64 products: a norm beyond fp32 has a coefficient below its normal range
-  for (int u = blockIdx.x; u < t.first[t.count]; u += gridDim.x) {
-    const int i = find(t, u);
-    const int64_t at = static_cast<int64_t>(u - t.first[i]) * kChunk, n = min(t.n[i] - at, static_cast<int64_t>(kChunk));
+  const int units = t.first[t.count];
+  if (static_cast<int>(blockIdx.x) >= units) return;
+  int i = find(t, units - 1 - blockIdx.x);
+  for (int u = units - 1 - blockIdx.x; u >= 0; u -= gridDim.x) {
+    while (t.first[i] > u) --i;
     if (!clip && t.out[i] == t.grad[i]) continue;
-    if (t.bf16[i >> 5] >> (i & 31) & 1) {
-      const uint16_t* g = static_cast<const uint16_t*>(t.grad[i]) + at;
-      uint16_t* o = static_cast<uint16_t*>(t.out[i]) + at;
-      for (int64_t j = threadIdx.x; j < n; j += kThreads) o[j] = clip ? static_cast<uint16_t>(cvt_pk_bf16(static_cast<float>(bf16_to_f32(g[j]) * c), 0.0f)) : g[j];
-    } else {
-      const float* g = static_cast<const float*>(t.grad[i]) + at;
-      float* o = static_cast<float*>(t.out[i]) + at;
-      for (int64_t j = threadIdx.x; j < n; j += kThreads) o[j] = clip ? static_cast<float>(g[j] * c) : g[j];
-    }
+    const int64_t at = static_cast<int64_t>(u - t.first[i]) * kUnit;
+    const int n = static_cast<int>(min(t.n[i] - at, static_cast<int64_t>(kUnit)));
+    if (t.bf16[i >> 5] >> (i & 31) & 1)
+      scale_unit(static_cast<const uint16_t*>(t.grad[i]) + at, static_cast<uint16_t*>(t.out[i]) + at, n, clip, c);
+    else
+      scale_unit(static_cast<const float*>(t.grad[i]) + at, static_cast<float*>(t.out[i]) + at, n, clip, c);
   }
 }
 
@@ -105,7 +175,7 @@ int fill(const GradTensor* g, int at, int n, Table* t) {
   for (uint32_t& b : t->bf16) b = 0;
   for (; i < kTable && at + i < n; ++i) {
     const GradTensor& s = g[at + i];
-    const int64_t u = (s.n + kChunk - 1) / kChunk;
+    const int64_t u = (s.n + kUnit - 1) / kUnit;
     t->grad[i] = s.grad;
     t->out[i] = s.out;
     t->n[i] = s.n;
@@ -120,7 +190,7 @@ int fill(const GradTensor* g, int at, int n, Table* t) {
 
 }  // namespace
 
-size_t grad_clip_workspace_bytes(int n) { return 256 + static_cast<size_t>(n / kTable + 2) * kMaxBlocks * sizeof(double); }
+size_t grad_clip_workspace_bytes(int n) { return 256 + static_cast<size_t>(n / kTable + 2) * kSquareBlocks * sizeof(double); }
 
 hipError_t launch_grad_clip(const GradTensor* g, int n, float max_norm, float* norm, void* workspace, hipStream_t stream) {
   double* const partial = static_cast<double*>(workspace);
@@ -128,14 +198,14 @@ hipError_t launch_grad_clip(const GradTensor* g, int n, float max_norm, float* n
   Table t{};
   for (int at = 0; at < n;) {
     const int taken = fill(g, at, n, &t);
-    const int blocks = std::min(t.first[t.count], kMaxBlocks);
+    const int blocks = std::min(t.first[t.count], kSquareBlocks);
     if (blocks > 0) grad_square_kernel<<<blocks, kThreads, 0, stream>>>(t, partial + partials);
     partials += blocks;
     at += taken;
   }
   for (int at = 0; at == 0 || at < n;) {
     const int taken = fill(g, at, n, &t);
-    const int blocks = std::max(std::min(t.first[t.count], kMaxBlocks), 1);
+    const int blocks = std::max(std::min(t.first[t.count], kScaleBlocks), 1);
     grad_scale_kernel<<<blocks, kThreads, 0, stream>>>(t, partial, partials, max_norm, norm);
     at += std::max(taken, 1);
   }

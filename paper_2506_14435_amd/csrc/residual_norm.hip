@@ -159,14 +159,16 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_kernel(Resi
   }
 }
 
-// Gradient.  The workgroup's sums for the parameters of a thread's channels stay in registers over its rows and leave as one
-// partial row per row slot: partial[(block * kRows + slot)][5][d], summed by residual_params_kernel.
+// Gradient.  A thread's sums for the parameters of its channels stay in registers over the rows of the workgroup; the row slots of
+// a workgroup meet in LDS, and the workgroup leaves one partial row for each parameter gradient that is asked for:
+// partial[block][which of `want`][d], summed by residual_params_kernel.  The next row is on its way while one is worked on.
 template <int NT, typename T>
 __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_kernel(ResidualArgs a, const T* __restrict__ r, const T* __restrict__ y,
                                                                                      const T* __restrict__ d_total, const T* __restrict__ d_normed,
-                                                                                     T* __restrict__ dr, T* __restrict__ dy, float* __restrict__ partial) {
+                                                                                     T* __restrict__ dr, T* __restrict__ dy, float* __restrict__ partial, int want) {
   constexpr int kRows = rows_of_block<NT>();
   __shared__ float s_buf[kRows][2 * (NT / 64)][2];
+  __shared__ float s_merge[kRows > 1 ? block_threads<NT>() * 8 : 1];
   const int slot = threadIdx.x / NT, c = (threadIdx.x % NT) * 8;
   const bool in = c < a.d;
   RowSum<NT> sum{s_buf[slot]};
@@ -175,20 +177,37 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
   load_param(a.post_beta, in, c, 0.0f, b_post);
   load_param(a.gate, in, c, 1.0f, gate);
   load_param(a.pre_gamma, in, c, 1.0f, g_pre);
-  float p_gate[8] = {}, p_post_g[8] = {}, p_post_b[8] = {}, p_pre_g[8] = {}, p_pre_b[8] = {};
+  float p[5][8] = {};   // gate, post gamma, post beta, pre gamma, pre beta
   const float inv_d = 1.0f / static_cast<float>(a.d);
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.T; row0 += static_cast<int64_t>(gridDim.x) * kRows) {
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
+  struct Raw {
+    Row8<T> y, r, n, t;
+  };
+  auto place = [&](int64_t row0) { return min(row0 + slot, static_cast<int64_t>(a.T) - 1) * a.d + c; };
+  auto load = [&](int64_t row0) __attribute__((always_inline)) {
+    Raw q;
+    const int64_t at = place(row0);
+    if (in) {
+      q.y.load(y + at);
+      q.r.load(r + at);
+      if (d_normed != nullptr) q.n.load(d_normed + at);
+      if (d_total != nullptr) q.t.load(d_total + at);
+    }
+    return q;
+  };
+  Raw next = load(static_cast<int64_t>(blockIdx.x) * kRows);
+  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.T; row0 += step) {
     const bool live = row0 + slot < a.T;
-    const int64_t at = min(row0 + slot, static_cast<int64_t>(a.T) - 1) * a.d + c;
+    const int64_t at = place(row0);
+    const Raw raw = next;
+    next = load(row0 + step);
+    __builtin_amdgcn_sched_barrier(0);
     float rv[8] = {}, hat_y[8] = {}, up[8] = {}, dn[8] = {};
     if (in) {
-      Row8<T> q;
-      q.load(y + at);
-      q.get(hat_y);
-      q.load(r + at);
-      q.get(rv);
-      if (d_normed != nullptr) { q.load(d_normed + at); q.get(dn); }
-      if (d_total != nullptr) { q.load(d_total + at); q.get(up); }
+      raw.y.get(hat_y);
+      raw.r.get(rv);
+      if (d_normed != nullptr) raw.n.get(dn);
+      if (d_total != nullptr) raw.t.get(up);
     }
     float z[8], inv_y = 1.0f;
     if (a.post_kind) {
@@ -208,8 +227,8 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (live) {
-          p_pre_g[i] = fmaf(dn[i], hat[i], p_pre_g[i]);
-          p_pre_b[i] += dn[i];
+          p[3][i] = fmaf(dn[i], hat[i], p[3][i]);
+          p[4][i] += dn[i];
         }
         dn[i] *= g_pre[i];
         m1 += dn[i];
@@ -231,7 +250,7 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float bu = in ? a.branch_scale * up[i] : 0.0f;
-      if (live) p_gate[i] = fmaf(bu, z[i], p_gate[i]);
+      if (live) p[0][i] = fmaf(bu, z[i], p[0][i]);
       dz[i] = bu * gate[i];
     }
     if (a.post_kind) {
@@ -239,8 +258,8 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (live) {
-          p_post_g[i] = fmaf(dz[i], hat_y[i], p_post_g[i]);
-          p_post_b[i] += dz[i];
+          p[1][i] = fmaf(dz[i], hat_y[i], p[1][i]);
+          p[2][i] += dz[i];
         }
         dz[i] *= g_post[i];
         m1 += dz[i];
@@ -254,25 +273,44 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
     }
     if (in && live) Row8<T>::store(dy + at, dz);
   }
-  if (partial != nullptr && in) {
-    float* const p = partial + (static_cast<int64_t>(blockIdx.x) * kRows + slot) * 5 * a.d + c;
-    Row8<float>::store(p, p_gate);
-    Row8<float>::store(p + a.d, p_post_g);
-    Row8<float>::store(p + 2 * a.d, p_post_b);
-    Row8<float>::store(p + 3 * a.d, p_pre_g);
-    Row8<float>::store(p + 4 * a.d, p_pre_b);
+  float* out = partial + static_cast<int64_t>(blockIdx.x) * __builtin_popcount(want) * a.d + c;
+#pragma unroll
+  for (int w = 0; w < 5; ++w) {
+    if (!(want >> w & 1)) continue;
+    if constexpr (kRows > 1) {
+      __syncthreads();
+      if (slot > 0) Row8<float>::store(s_merge + threadIdx.x * 8, p[w]);
+      __syncthreads();
+      if (slot == 0)
+#pragma unroll
+        for (int k = 1; k < kRows; ++k)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[w][i] += s_merge[(threadIdx.x + k * NT) * 8 + i];
+    }
+    if (slot == 0 && in) Row8<float>::store(out, p[w]);
+    out += a.d;
   }
 }
 
-// Sums of the partial rows in their order: 64 columns per workgroup, 16 slices of the rows.
-__global__ __launch_bounds__(1024) void residual_params_kernel(const float* __restrict__ partial, int rows, int d, ResidualGrads out) {
+// Sums of the partial rows in their order: 64 columns of a parameter gradient per workgroup, 16 slices of the rows.
+__global__ __launch_bounds__(1024) void residual_params_kernel(const float* __restrict__ partial, int rows, int d, int want, ResidualGrads out) {
   __shared__ float s_p[16][64];
-  const int which = blockIdx.y, c = blockIdx.x * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6;
-  float* const dst = which == 0 ? out.gate : which == 1 ? out.post_gamma : which == 2 ? out.post_beta : which == 3 ? out.pre_gamma : out.pre_beta;
-  if (dst == nullptr) return;
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63), part = threadIdx.x >> 6, n = gridDim.y;
+  float* const all[5] = {out.gate, out.post_gamma, out.post_beta, out.pre_gamma, out.pre_beta};
+  float* dst = nullptr;
+  int k = blockIdx.y;
+#pragma unroll
+  for (int w = 0; w < 5; ++w)
+    if (want >> w & 1) {
+      if (k == 0) dst = all[w];
+      --k;
+    }
   float s = 0.0f;
-  if (c < d)
-    for (int i = part; i < rows; i += 16) s += partial[(static_cast<int64_t>(i) * 5 + which) * d + c];
+  if (c < d) {
+    const float* const p = partial + static_cast<int64_t>(blockIdx.y) * d + c;
+#pragma unroll 16
+    for (int i = part; i < rows; i += 16) s += p[static_cast<int64_t>(i) * n * d];
+  }
   s_p[part][threadIdx.x & 63] = s;
   __syncthreads();
   if (part == 0 && c < d) {
@@ -295,17 +333,19 @@ int threads_of_row(int d) {
   while (nt * 8 < d) nt *= 2;
   return nt;
 }
+// Two workgroups of 256 threads per CU (as many threads for wider rows), at least two rows for each slot: every workgroup leaves a
+// partial row.
 int backward_blocks(int T, int d) {
-  const int rows = std::max(256 / threads_of_row(d), 1);
-  return std::min((T + rows - 1) / rows, 512);
+  const int nt = threads_of_row(d), rows = std::max(256 / nt, 1);
+  return std::max(std::min((T + 2 * rows - 1) / (2 * rows), 512 * 256 / std::max(nt, 256)), 1);
 }
 
 template <int NT, typename T>
 void backward(const ResidualArgs& a, const void* r, const void* y, const void* d_total, const void* d_normed, void* dr, void* dy, float* partial,
-              hipStream_t stream) {
+              int want, hipStream_t stream) {
   residual_norm_backward_kernel<NT, T><<<backward_blocks(a.T, a.d), block_threads<NT>(), 0, stream>>>(
       a, static_cast<const T*>(r), static_cast<const T*>(y), static_cast<const T*>(d_total), static_cast<const T*>(d_normed), static_cast<T*>(dr),
-      static_cast<T*>(dy), partial);
+      static_cast<T*>(dy), partial, want);
 }
 
 }  // namespace
@@ -327,24 +367,23 @@ hipError_t launch_residual_norm(const ResidualArgs& a, bool f32, const void* r, 
 }
 
 size_t residual_norm_workspace_bytes(int T, int d) {
-  const size_t rows = static_cast<size_t>(backward_blocks(std::max(T, 1), d)) * std::max(256 / threads_of_row(d), 1);
-  return 256 + rows * 5 * d * sizeof(float);
+  return 256 + static_cast<size_t>(backward_blocks(std::max(T, 1), d)) * 5 * d * sizeof(float);
 }
 
 hipError_t launch_residual_norm_backward(const ResidualArgs& a, bool f32, const void* r, const void* y, const void* d_total, const void* d_normed, void* dr,
                                          void* dy, const ResidualGrads& grads, void* workspace, hipStream_t stream) {
-  const bool params = grads.gate || grads.post_gamma || grads.post_beta || grads.pre_gamma || grads.pre_beta;
-  float* const partial = params ? static_cast<float*>(workspace) : nullptr;
+  const int want = (grads.gate ? 1 : 0) | (grads.post_gamma ? 2 : 0) | (grads.post_beta ? 4 : 0) | (grads.pre_gamma ? 8 : 0) | (grads.pre_beta ? 16 : 0);
+  float* const partial = static_cast<float*>(workspace);
   int rows = 0;
   if (a.T > 0) {
-    rows = backward_blocks(a.T, a.d) * std::max(256 / threads_of_row(a.d), 1);
+    rows = backward_blocks(a.T, a.d);
 #define MOTE_CALL(NT)                                                                                      \
-  f32 ? backward<NT, float>(a, r, y, d_total, d_normed, dr, dy, partial, stream)                            \
-      : backward<NT, uint16_t>(a, r, y, d_total, d_normed, dr, dy, partial, stream)
+  f32 ? backward<NT, float>(a, r, y, d_total, d_normed, dr, dy, partial, want, stream)                      \
+      : backward<NT, uint16_t>(a, r, y, d_total, d_normed, dr, dy, partial, want, stream)
     MOTE_ROW_DISPATCH(MOTE_CALL)
 #undef MOTE_CALL
   }
-  if (params) residual_params_kernel<<<dim3((a.d + 63) / 64, 5), 1024, 0, stream>>>(partial, rows, a.d, grads);
+  if (want) residual_params_kernel<<<dim3((a.d + 63) / 64, __builtin_popcount(want)), 1024, 0, stream>>>(partial, rows, a.d, want, grads);
   return hipGetLastError();
 }
 
