@@ -444,26 +444,33 @@ def mote_layer_forward_static(layer: MoteLayer, x: torch.Tensor, out: torch.Tens
     return out
 
 
-class _on_device:
-    """The device of the given tensors (all on one) as the current one for a library call, whatever the caller's is."""
+def _one_device(**tensors) -> int:
+    """Number of the device that all given tensors are on."""
+    dev = None
+    for name, t in tensors.items():
+        if t is not None:
+            n = t.get_device()
+            if dev is None:
+                dev = n
+            elif n != dev:
+                raise MoteError(f"{name} is on device {n}, the other tensors are on {dev}")
+    return dev
 
-    def __init__(self, **tensors):
-        dev = None
-        for name, t in tensors.items():
-            if t is None:
-                continue
-            dev = t.device if dev is None else dev
-            if t.device != dev:
-                raise MoteError(f"{name} is on {t.device}, the other tensors are on {dev}")
-        self._guard = None if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
 
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
+def _call(name: str, dev: int, *args) -> None:
+    """Library call `name` on the current stream of device `dev`, whatever device is the current one."""
+    fn = getattr(load_library(), name)
+    if dev == torch.cuda.current_device():
+        status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+    if status != 0:
+        _check(status, name)
 
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _shape(t: torch.Tensor, shape, name: str) -> torch.Tensor:
@@ -480,7 +487,6 @@ def mote_layer_forward_routed(layer: MoteLayer, x: torch.Tensor, topk_idx: torch
                               out: torch.Tensor = None, taps: dict = None, workspace: torch.Tensor = None) -> torch.Tensor:
     """mote_layer_forward on a given routing (topk_idx int32, topk_w fp32 [T, k], e.g. of mote_route) instead of the layer's
     router; a slot whose index is outside 0 .. E - 1 adds nothing."""
-    lib = load_library()
     _dev(x, torch.bfloat16, "x")
     n_tok = x.shape[0]
     _shape(x, (n_tok, layer.d_model), "x")
@@ -489,15 +495,14 @@ def mote_layer_forward_routed(layer: MoteLayer, x: torch.Tensor, topk_idx: torch
     if out is None:
         out = torch.empty_like(x)
     _shape(_dev(out, torch.bfloat16, "out"), x.shape, "out")
-    with _on_device(x=x, topk_idx=topk_idx, topk_w=topk_w, out=out, w_router=layer.tensors["w_router"], workspace=workspace):
-        if workspace is None:
-            workspace = layer.workspace(max(n_tok, 1))
-        ts = None
-        if taps is not None:
-            ts = MoteTapsStruct(*[taps[n].data_ptr() if n in taps else None for n in TAP_FIELDS])
-        _check(lib.mote_layer_forward_routed(ctypes.byref(layer.struct), _ptr(x), n_tok, _ptr(topk_idx), _ptr(topk_w), _ptr(out),
-                                             _ptr(workspace), workspace.numel(), ctypes.byref(ts) if ts is not None else None,
-                                             _stream()), "mote_layer_forward_routed")
+    dev = _one_device(x=x, topk_idx=topk_idx, topk_w=topk_w, out=out, w_router=layer.tensors["w_router"], workspace=workspace)
+    if workspace is None:
+        workspace = layer.workspace(max(n_tok, 1))
+    ts = None
+    if taps is not None:
+        ts = MoteTapsStruct(*[taps[n].data_ptr() if n in taps else None for n in TAP_FIELDS])
+    _call("mote_layer_forward_routed", dev, ctypes.byref(layer.struct), _addr(x), n_tok, _addr(topk_idx), _addr(topk_w), _addr(out),
+          _addr(workspace), workspace.numel(), ctypes.byref(ts) if ts is not None else None)
     return out
 
 
@@ -540,24 +545,23 @@ def mote_route(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRouting, se
                token_mask: torch.Tensor = None, want_logits: bool = False, want_stats: bool = False,
                workspace: torch.Tensor = None) -> Routed:
     """Scored routing of x bf16 [T, d] by w_router bf16 [d, E]; select_bias fp32 [E], token_mask bool or uint8 [T] (0: padding)."""
-    lib = load_library()
     n_tok, d, n_exp, token_mask = _router_operands(x, w_router, token_mask)
     if select_bias is not None:
         _shape(_dev(select_bias, torch.float32, "select_bias"), (n_exp,), "select_bias")
-    with _on_device(x=x, w_router=w_router, select_bias=select_bias, token_mask=token_mask, workspace=workspace):
-        dev, k = x.device, routing.top_k
-        idx = torch.empty(n_tok, k, dtype=torch.int32, device=dev)
-        wt = torch.empty(n_tok, k, dtype=torch.float32, device=dev)
-        logits = torch.empty(n_tok, n_exp, dtype=torch.float32, device=dev) if want_logits else None
-        counts = score_sum = None
-        if want_stats:
-            counts = torch.empty(n_exp, dtype=torch.int32, device=dev)
-            score_sum = torch.empty(n_exp, dtype=torch.float32, device=dev)
-        if want_stats or n_tok > 64:
-            workspace = _workspace(workspace, lib.mote_route_workspace_bytes(n_tok, d, n_exp), dev)
-        _check(lib.mote_route(ctypes.byref(routing.struct), _ptr(x), _ptr(w_router), _ptr(select_bias), _ptr(token_mask), n_tok, d,
-                              n_exp, _ptr(idx), _ptr(wt), _ptr(logits), _ptr(counts), _ptr(score_sum), _ptr(workspace),
-                              workspace.numel() if workspace is not None else 0, _stream()), "mote_route")
+    n = _one_device(x=x, w_router=w_router, select_bias=select_bias, token_mask=token_mask, workspace=workspace)
+    dev, k = x.device, routing.top_k
+    idx = torch.empty(n_tok, k, dtype=torch.int32, device=dev)
+    wt = torch.empty(n_tok, k, dtype=torch.float32, device=dev)
+    logits = torch.empty(n_tok, n_exp, dtype=torch.float32, device=dev) if want_logits else None
+    counts = score_sum = None
+    if want_stats:
+        counts = torch.empty(n_exp, dtype=torch.int32, device=dev)
+        score_sum = torch.empty(n_exp, dtype=torch.float32, device=dev)
+    if want_stats or n_tok > 64:
+        workspace = _workspace(workspace, load_library().mote_route_workspace_bytes(n_tok, d, n_exp), dev)
+    _call("mote_route", n, ctypes.byref(routing.struct), _addr(x), _addr(w_router), _addr(select_bias), _addr(token_mask), n_tok, d,
+          n_exp, _addr(idx), _addr(wt), _addr(logits), _addr(counts), _addr(score_sum), _addr(workspace),
+          workspace.numel() if workspace is not None else 0)
     return Routed(idx, wt, logits, counts, score_sum)
 
 
@@ -566,22 +570,21 @@ def mote_route_backward(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRo
                         token_mask: torch.Tensor = None, want_dx: bool = True, want_dw: bool = True,
                         workspace: torch.Tensor = None):
     """Gradients of mote_route: (dx fp32 [T, d], dw_router fp32 [d, E]) for d_topk_w fp32 [T, k] and d_score_sum fp32 [E]."""
-    lib = load_library()
     n_tok, d, n_exp, token_mask = _router_operands(x, w_router, token_mask)
     _shape(_dev(logits, torch.float32, "logits"), (n_tok, n_exp), "logits")
     _shape(_dev(topk_idx, torch.int32, "topk_idx"), (n_tok, routing.top_k), "topk_idx")
     _shape(_dev(d_topk_w, torch.float32, "d_topk_w"), (n_tok, routing.top_k), "d_topk_w")
     if d_score_sum is not None:
         _shape(_dev(d_score_sum, torch.float32, "d_score_sum"), (n_exp,), "d_score_sum")
-    with _on_device(x=x, w_router=w_router, logits=logits, topk_idx=topk_idx, d_topk_w=d_topk_w, d_score_sum=d_score_sum,
-                    token_mask=token_mask, workspace=workspace):
-        dev = x.device
-        dx = torch.empty(n_tok, d, dtype=torch.float32, device=dev) if want_dx else None
-        dw = torch.empty(d, n_exp, dtype=torch.float32, device=dev) if want_dw else None
-        workspace = _workspace(workspace, lib.mote_route_backward_workspace_bytes(n_tok, d, n_exp), dev)
-        _check(lib.mote_route_backward(ctypes.byref(routing.struct), _ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx),
-                                       _ptr(d_topk_w), _ptr(d_score_sum), _ptr(token_mask), n_tok, d, n_exp, _ptr(dx), _ptr(dw),
-                                       _ptr(workspace), workspace.numel(), _stream()), "mote_route_backward")
+    n = _one_device(x=x, w_router=w_router, logits=logits, topk_idx=topk_idx, d_topk_w=d_topk_w, d_score_sum=d_score_sum,
+                    token_mask=token_mask, workspace=workspace)
+    dev = x.device
+    dx = torch.empty(n_tok, d, dtype=torch.float32, device=dev) if want_dx else None
+    dw = torch.empty(d, n_exp, dtype=torch.float32, device=dev) if want_dw else None
+    workspace = _workspace(workspace, load_library().mote_route_backward_workspace_bytes(n_tok, d, n_exp), dev)
+    _call("mote_route_backward", n, ctypes.byref(routing.struct), _addr(x), _addr(w_router), _addr(logits), _addr(topk_idx),
+          _addr(d_topk_w), _addr(d_score_sum), _addr(token_mask), n_tok, d, n_exp, _addr(dx), _addr(dw), _addr(workspace),
+          workspace.numel())
     return dx, dw
 
 
@@ -609,8 +612,9 @@ class MoteResidual:
                                          gate.data_ptr() if gate is not None else None, residual_scale, branch_scale,
                                          ctypes.pointer(pre.struct) if pre is not None else None)
 
-    def _tensors(self):
-        return dict(post_gamma=self.post and self.post.gamma, gate=self.gate, pre_gamma=self.pre and self.pre.gamma)
+        params = [p for p in (gate, post and post.gamma, post and post.beta, pre and pre.gamma, pre and pre.beta) if p is not None]
+        _one_device(**{f"parameter {i}": p for i, p in enumerate(params)})
+        self._param = params[0] if params else None   # says where the parameters are
 
 
 def _residual_operands(block: MoteResidual, **tensors):
@@ -627,16 +631,14 @@ def _residual_operands(block: MoteResidual, **tensors):
 def mote_residual_norm(block: MoteResidual, r: torch.Tensor, y: torch.Tensor, total: torch.Tensor = None,
                        normed: torch.Tensor = None):
     """(total, normed) of the residual stream r and the branch output y, bf16 or fp32 [T, d]; normed is None without a pre norm."""
-    lib = load_library()
     if block.pre is None and normed is not None:
         raise MoteError("normed needs a block with a pre norm")
     n_tok, dt = _residual_operands(block, r=r, y=y, total=total, normed=normed)
-    with _on_device(r=r, y=y, total=total, normed=normed, **block._tensors()):
-        total = torch.empty_like(r) if total is None else total
-        if normed is None and block.pre is not None:
-            normed = torch.empty_like(r)
-        _check(lib.mote_residual_norm(ctypes.byref(block.struct), _ptr(r), _ptr(y), dt, n_tok, block.d, _ptr(total), _ptr(normed),
-                                      _stream()), "mote_residual_norm")
+    dev = _one_device(r=r, y=y, total=total, normed=normed, parameters=block._param)
+    total = torch.empty_like(r) if total is None else total
+    if normed is None and block.pre is not None:
+        normed = torch.empty_like(r)
+    _call("mote_residual_norm", dev, ctypes.byref(block.struct), _addr(r), _addr(y), dt, n_tok, block.d, _addr(total), _addr(normed))
     return total, normed
 
 
@@ -655,19 +657,17 @@ def mote_residual_norm_backward(block: MoteResidual, r: torch.Tensor, y: torch.T
                                 d_normed: torch.Tensor = None, want_params: bool = True,
                                 workspace: torch.Tensor = None) -> ResidualGrads:
     """Gradients of mote_residual_norm(block, r, y) for the gradients of its outputs (None: zero)."""
-    lib = load_library()
     n_tok, dt = _residual_operands(block, r=r, y=y, d_total=d_total, d_normed=d_normed)
-    with _on_device(r=r, y=y, d_total=d_total, d_normed=d_normed, workspace=workspace, **block._tensors()):
-        dev = r.device
-        dr, dy = torch.empty_like(r), torch.empty_like(y)
-        has = (block.gate is not None, block.post is not None, block.post is not None and block.post.beta is not None,
-               block.pre is not None, block.pre is not None and block.pre.beta is not None)
-        par = [torch.empty(block.d, dtype=torch.float32, device=dev) if h and want_params else None for h in has]
-        workspace = _workspace(workspace, lib.mote_residual_norm_workspace_bytes(ctypes.byref(block.struct), n_tok, block.d), dev)
-        grads = MoteResidualGradsStruct(*[p.data_ptr() if p is not None else None for p in par])
-        _check(lib.mote_residual_norm_backward(ctypes.byref(block.struct), _ptr(r), _ptr(y), _ptr(d_total), _ptr(d_normed), dt, n_tok,
-                                               block.d, _ptr(dr), _ptr(dy), ctypes.byref(grads), _ptr(workspace),
-                                               workspace.numel(), _stream()), "mote_residual_norm_backward")
+    n = _one_device(r=r, y=y, d_total=d_total, d_normed=d_normed, workspace=workspace, parameters=block._param)
+    dev = r.device
+    dr, dy = torch.empty_like(r), torch.empty_like(y)
+    has = (block.gate is not None, block.post is not None, block.post is not None and block.post.beta is not None,
+           block.pre is not None, block.pre is not None and block.pre.beta is not None)
+    par = [torch.empty(block.d, dtype=torch.float32, device=dev) if h and want_params else None for h in has]
+    workspace = _workspace(workspace, load_library().mote_residual_norm_workspace_bytes(ctypes.byref(block.struct), n_tok, block.d), dev)
+    grads = MoteResidualGradsStruct(*[_addr(p) for p in par])
+    _call("mote_residual_norm_backward", n, ctypes.byref(block.struct), _addr(r), _addr(y), _addr(d_total), _addr(d_normed), dt, n_tok,
+          block.d, _addr(dr), _addr(dy), ctypes.byref(grads), _addr(workspace), workspace.numel())
     return ResidualGrads(dr, dy, *par)
 
 
@@ -697,12 +697,10 @@ class GradClip:
 def mote_clip_grad_norm(clip: GradClip, max_norm: float, norm: torch.Tensor = None) -> torch.Tensor:
     """Scales the gradients of `clip` to a global norm of at most max_norm; returns that norm before the scaling (fp32 [1]).
     Calls on one GradClip share its workspace: they must be ordered on one stream."""
-    lib = load_library()
-    dev = clip.grads[0].device
-    with _on_device(grad=clip.grads[0], norm=norm):
-        norm = torch.empty(1, dtype=torch.float32, device=dev) if norm is None else _shape(_dev(norm, torch.float32, "norm"), (1,), "norm")
-        _check(lib.mote_clip_grad_norm(clip.descriptors, len(clip.grads), max_norm, _ptr(norm), _ptr(clip.workspace),
-                                       clip.workspace.numel(), _stream()), "mote_clip_grad_norm")
+    dev = _one_device(grad=clip.grads[0], norm=norm)
+    norm = torch.empty(1, dtype=torch.float32, device=clip.grads[0].device) if norm is None else _shape(_dev(norm, torch.float32, "norm"), (1,), "norm")
+    _call("mote_clip_grad_norm", dev, clip.descriptors, len(clip.grads), max_norm, _addr(norm), _addr(clip.workspace),
+          clip.workspace.numel())
     return norm
 
 

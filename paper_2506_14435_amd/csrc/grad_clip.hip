@@ -16,8 +16,9 @@ namespace {
 
 constexpr int kTable = 120;             // tensors of a launch: 3.8 KB of kernel arguments
 constexpr int kThreads = 256;
-constexpr int kUnit = 4096;             // elements of a unit of work: 64 (bf16: 32) bytes a thread, all on their way together
-constexpr int kSquareBlocks = 1024, kScaleBlocks = 2048;   // workgroups of a launch at most
+constexpr int kUnit = 8192;             // elements of a unit of work: 128 (bf16: 64) bytes a thread, all on their way together
+constexpr int kPart = kUnit / 2;        // of a unit that is scaled
+constexpr int kSquareBlocks = 2048, kScaleBlocks = 2048;   // workgroups of a launch at most
 struct Table {
   const void* grad[kTable];
   void* out[kTable];
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void grad_square_kernel(const Table t, do
 // c == 1: a copy, bits as they are
 template <typename T>
 __device__ __forceinline__ void scale_unit(const T* g, T* o, int n, bool clip, double c) {
-  constexpr int N = Vec<T>::N, V = kUnit / N / kThreads;
+  constexpr int N = Vec<T>::N, V = kPart / N / kThreads;
   if ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(o)) % 16 == 0) {
     const u4* const p = reinterpret_cast<const u4*>(g);
     u4* const q = reinterpret_cast<u4*>(o);
@@ -161,10 +162,13 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(const Table t, con
     if (!clip && t.out[i] == t.grad[i]) continue;
     const int64_t at = static_cast<int64_t>(u - t.first[i]) * kUnit;
     const int n = static_cast<int>(min(t.n[i] - at, static_cast<int64_t>(kUnit)));
-    if (t.bf16[i >> 5] >> (i & 31) & 1)
-      scale_unit(static_cast<const uint16_t*>(t.grad[i]) + at, static_cast<uint16_t*>(t.out[i]) + at, n, clip, c);
-    else
-      scale_unit(static_cast<const float*>(t.grad[i]) + at, static_cast<float*>(t.out[i]) + at, n, clip, c);
+    const bool bf16 = t.bf16[i >> 5] >> (i & 31) & 1;
+#pragma unroll 1
+    for (int h = 0; h < n; h += kPart) {
+      const int m = min(n - h, kPart);
+      if (bf16) scale_unit(static_cast<const uint16_t*>(t.grad[i]) + at + h, static_cast<uint16_t*>(t.out[i]) + at + h, m, clip, c);
+      else scale_unit(static_cast<const float*>(t.grad[i]) + at + h, static_cast<float*>(t.out[i]) + at + h, m, clip, c);
+    }
   }
 }
 

@@ -177,17 +177,18 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
   load_param(a.post_beta, in, c, 0.0f, b_post);
   load_param(a.gate, in, c, 1.0f, gate);
   load_param(a.pre_gamma, in, c, 1.0f, g_pre);
-  float p[5][8] = {};   // gate, post gamma, post beta, pre gamma, pre beta
+#pragma unroll
+  for (int i = 0; i < 8; ++i) gate[i] *= a.branch_scale;
+  float p[5][8] = {};   // gate (without the branch scale), post gamma, post beta, pre gamma, pre beta
   const float inv_d = 1.0f / static_cast<float>(a.d);
   const int64_t step = static_cast<int64_t>(gridDim.x) * kRows;
   struct Raw {
     Row8<T> y, r, n, t;
   };
-  auto place = [&](int64_t row0) { return min(row0 + slot, static_cast<int64_t>(a.T) - 1) * a.d + c; };
-  auto load = [&](int64_t row0) __attribute__((always_inline)) {
+  auto load = [&](int64_t row) __attribute__((always_inline)) {
     Raw q;
-    const int64_t at = place(row0);
     if (in) {
+      const int64_t at = min(row, static_cast<int64_t>(a.T) - 1) * a.d + c;
       q.y.load(y + at);
       q.r.load(r + at);
       if (d_normed != nullptr) q.n.load(d_normed + at);
@@ -195,21 +196,24 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
     }
     return q;
   };
-  Raw next = load(static_cast<int64_t>(blockIdx.x) * kRows);
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * kRows; row0 < a.T; row0 += step) {
-    const bool live = row0 + slot < a.T;
-    const int64_t at = place(row0);
+  constexpr bool kAhead = NT < 1024;   // 128 registers a thread have no room for a second row
+  int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + slot;
+  Raw next = load(row);
+  for (; row - slot < a.T; row += step) {
     const Raw raw = next;
-    next = load(row0 + step);
-    __builtin_amdgcn_sched_barrier(0);
-    float rv[8] = {}, hat_y[8] = {}, up[8] = {}, dn[8] = {};
-    if (in) {
+    if constexpr (kAhead) {
+      next = load(row + step);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const bool store = in && row < a.T;
+    const int64_t at = row * a.d + c;
+    float hat_y[8] = {}, z[8], up[8] = {}, hat[8] = {}, dn[8] = {}, inv_y = 1.0f;
+    if (store) {   // a row behind the last is zeros: nothing of it reaches a sum
       raw.y.get(hat_y);
-      raw.r.get(rv);
+      raw.r.get(hat);
       if (d_normed != nullptr) raw.n.get(dn);
       if (d_total != nullptr) raw.t.get(up);
     }
-    float z[8], inv_y = 1.0f;
     if (a.post_kind) {
       inv_y = normalise(sum, a.post_kind, a.post_eps, inv_d, in, hat_y);
 #pragma unroll
@@ -219,60 +223,59 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
       for (int i = 0; i < 8; ++i) z[i] = hat_y[i];
     }
     if (d_normed != nullptr) {
-      float hat[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) hat[i] = fmaf(a.residual_scale, rv[i], a.branch_scale * (gate[i] * z[i]));
+      for (int i = 0; i < 8; ++i) hat[i] = fmaf(gate[i], z[i], a.residual_scale * hat[i]);
       const float inv = normalise(sum, a.pre_kind, a.pre_eps, inv_d, in, hat);
       float m1 = 0.0f, m2 = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (live) {
-          p[3][i] = fmaf(dn[i], hat[i], p[3][i]);
-          p[4][i] += dn[i];
-        }
+        p[3][i] = fmaf(dn[i], hat[i], p[3][i]);
+        p[4][i] += dn[i];
         dn[i] *= g_pre[i];
         m1 += dn[i];
         m2 = fmaf(dn[i], hat[i], m2);
       }
       sum(m1, m2);
-      m1 = a.pre_kind == 2 ? m1 * inv_d : 0.0f;
-      m2 *= inv_d;
+      m1 = a.pre_kind == 2 ? m1 * inv_d * inv : 0.0f;
+      m2 *= inv_d * inv;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) up[i] = fmaf(inv, dn[i] - m1 - hat[i] * m2, up[i]);
+      for (int i = 0; i < 8; ++i) up[i] = fmaf(inv, dn[i], up[i] - fmaf(hat[i], m2, m1));
     }
-    if (in && live) {
+    if (store) {
       float o[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) o[i] = a.residual_scale * up[i];
       Row8<T>::store(dr + at, o);
     }
-    float dz[8];
+    if (!in)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) up[i] = 0.0f;   // the mean of a layer norm's gradient reaches channels beyond d
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float bu = in ? a.branch_scale * up[i] : 0.0f;
-      if (live) p[0][i] = fmaf(bu, z[i], p[0][i]);
-      dz[i] = bu * gate[i];
+      p[0][i] = fmaf(up[i], z[i], p[0][i]);
+      up[i] *= gate[i];
     }
     if (a.post_kind) {
       float m1 = 0.0f, m2 = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (live) {
-          p[1][i] = fmaf(dz[i], hat_y[i], p[1][i]);
-          p[2][i] += dz[i];
-        }
-        dz[i] *= g_post[i];
-        m1 += dz[i];
-        m2 = fmaf(dz[i], hat_y[i], m2);
+        p[1][i] = fmaf(up[i], hat_y[i], p[1][i]);
+        p[2][i] += up[i];
+        up[i] *= g_post[i];
+        m1 += up[i];
+        m2 = fmaf(up[i], hat_y[i], m2);
       }
       sum(m1, m2);
-      m1 = a.post_kind == 2 ? m1 * inv_d : 0.0f;
-      m2 *= inv_d;
+      m1 = a.post_kind == 2 ? m1 * inv_d * inv_y : 0.0f;
+      m2 *= inv_d * inv_y;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) dz[i] = inv_y * (dz[i] - m1 - hat_y[i] * m2);
+      for (int i = 0; i < 8; ++i) up[i] = fmaf(inv_y, up[i], -fmaf(hat_y[i], m2, m1));
     }
-    if (in && live) Row8<T>::store(dy + at, dz);
+    if (store) Row8<T>::store(dy + at, up);
+    if constexpr (!kAhead) next = load(row + step);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p[0][i] *= a.branch_scale;
   float* out = partial + static_cast<int64_t>(blockIdx.x) * __builtin_popcount(want) * a.d + c;
 #pragma unroll
   for (int w = 0; w < 5; ++w) {
@@ -333,17 +336,19 @@ int threads_of_row(int d) {
   while (nt * 8 < d) nt *= 2;
   return nt;
 }
-// Two workgroups of 256 threads per CU (as many threads for wider rows), at least two rows for each slot: every workgroup leaves a
-// partial row.
-int backward_blocks(int T, int d) {
+// As many workgroups as the registers let reside (158 of them a thread for bf16, 186 for fp32: three and two workgroups of
+// 256 threads per CU), at least two rows for each slot: every workgroup leaves a partial row.  (8191 x 2048 bf16, the rows'
+// kernel and the sums behind it: two 57.3 + 4.8 us, three 49.0 + 6.2.)
+int backward_blocks(int T, int d, bool f32) {
   const int nt = threads_of_row(d), rows = std::max(256 / nt, 1);
-  return std::max(std::min((T + 2 * rows - 1) / (2 * rows), 512 * 256 / std::max(nt, 256)), 1);
+  const int most = std::max((f32 ? 512 : 768) * 256 / std::max(nt, 256), 256);
+  return std::max(std::min((T + 2 * rows - 1) / (2 * rows), most), 1);
 }
 
 template <int NT, typename T>
 void backward(const ResidualArgs& a, const void* r, const void* y, const void* d_total, const void* d_normed, void* dr, void* dy, float* partial,
               int want, hipStream_t stream) {
-  residual_norm_backward_kernel<NT, T><<<backward_blocks(a.T, a.d), block_threads<NT>(), 0, stream>>>(
+  residual_norm_backward_kernel<NT, T><<<backward_blocks(a.T, a.d, sizeof(T) == 4), block_threads<NT>(), 0, stream>>>(
       a, static_cast<const T*>(r), static_cast<const T*>(y), static_cast<const T*>(d_total), static_cast<const T*>(d_normed), static_cast<T*>(dr),
       static_cast<T*>(dy), partial, want);
 }
@@ -367,7 +372,7 @@ hipError_t launch_residual_norm(const ResidualArgs& a, bool f32, const void* r, 
 }
 
 size_t residual_norm_workspace_bytes(int T, int d) {
-  return 256 + static_cast<size_t>(backward_blocks(std::max(T, 1), d)) * 5 * d * sizeof(float);
+  return 256 + static_cast<size_t>(backward_blocks(std::max(T, 1), d, false)) * 5 * d * sizeof(float);
 }
 
 hipError_t launch_residual_norm_backward(const ResidualArgs& a, bool f32, const void* r, const void* y, const void* d_total, const void* d_normed, void* dr,
@@ -376,7 +381,7 @@ hipError_t launch_residual_norm_backward(const ResidualArgs& a, bool f32, const 
   float* const partial = static_cast<float*>(workspace);
   int rows = 0;
   if (a.T > 0) {
-    rows = backward_blocks(a.T, a.d);
+    rows = backward_blocks(a.T, a.d, f32);
 #define MOTE_CALL(NT)                                                                                      \
   f32 ? backward<NT, float>(a, r, y, d_total, d_normed, dr, dy, partial, want, stream)                      \
       : backward<NT, uint16_t>(a, r, y, d_total, d_normed, dr, dy, partial, want, stream)
