@@ -21,11 +21,12 @@ constexpr int kRtWaves = 8;
 constexpr int kRtThreads = 64 * kRtWaves;
 constexpr int kRtUnit = 64;       // channels of a unit
 constexpr int kRtRow = 65;        // elements of an LDS row of 64 logits or keys: the rows of a wavefront's four tokens start in different banks
-// How far a logit may be off, in units of 2^-24 |x| |w| (Euclidean norms, which bound sum |x w|): a unit is a chain of four
-// instructions, each of which aligns 16 products and the addend to the largest of them.  Measured at most 6.9 units of the
-// unit's own sum |x w| over normal, one-signed, wide-range and one-large inputs (1.9 for normal ones, and the errors of the
-// units of a row add up like random signs); taken as 8 in every unit, plus the rounding of the logit to fp32.
-constexpr float kRtBound = (8 + 1) * 0x1p-24f * 1.02f;
+// How far a logit may be off, in units of 2^-24 |x| |w| (Euclidean norms, which bound sum |x w|).  A unit is a chain of four
+// instructions, each of which aligns 16 products and the addend to the largest of them.  Measured against the unit's own
+// |x| |w|, over normal, one-signed, wide-range and one-large inputs: at most 6.0 units (1.3 for normal ones), of which at most
+// 1.6 have one sign in all units of a row; the rest adds up like random signs.  Taken: 3 for the first and 6 / sqrt(units) for
+// the second, plus one for the rounding of the logit to fp32.
+__device__ __forceinline__ float logit_bound(int units) { return (4.0f + 6.0f * __builtin_amdgcn_rsqf(static_cast<float>(units))) * 0x1p-24f * 1.02f; }
 
 // LDS written and read by lanes of one wavefront
 __device__ __forceinline__ void wave_lds_fence() {
@@ -113,11 +114,12 @@ __device__ __forceinline__ void route_scores(const RouteArgs& a, const double* l
 }
 
 // Selection for one token by the 16 lanes of a DPP row, on fp32 keys; the selected experts go to sel[0 .. k), which the caller
-// has filled with -1.  Returns the experts (bit v: s + 16 v) whose logits have to be settled because keys that decide are
-// too close: logits are off by `tol`, scores by the rounding of exp_of and rcp.  Bit 4: groups or equal keys are among them.
-// key_row, grp_row: 64 integers of LDS each (groups only), m_row: 8.
+// has filled with -1, and the first one that is not to sel[k].  Returns in every lane of the row: 0, the selection is final; j in
+// 1 .. k, only the experts sel[j - 1] and sel[j] are too close to be told apart; -1, more hangs on logits that are off by
+// `tol` and scores by the rounding of exp_of and rcp.
+// key_row, grp_row: 64 integers of LDS each (groups only).
 __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_row, const float (&sc)[4], double shift, int* key_row, int* grp_row,
-                                            int* m_row, int* sel, float tol) {
+                                            int* sel, float tol) {
   const int s = threadIdx.x & 15, E = a.E;
   const bool by_logit = keys_are_logits(a);
   float delta = key_tolerance(a, tol);
@@ -132,8 +134,7 @@ __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_
     if (f != f) f = -FLT_MAX;
     key[v] = f > -INFINITY ? order_of(f) : kNoKey;
   }
-  bool close = false, grouped = false;
-  int more = 0;
+  bool many = false;
   if (a.n_groups > 1) {
     const int G = a.n_groups, n = E / G;
 #pragma unroll
@@ -185,22 +186,11 @@ __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_
     best_out = row_max(best_out);
     const float width = 2.0f * static_cast<float>(a.group_top) * delta;
     const unsigned inv_n = 65536u / static_cast<unsigned>(n) + 1u;   // e / n for e < 64
-    if (best_out != kNoKey && near_keys(value_of(worst_in), value_of(best_out), width, slack)) {   // the groups around the border
-      close = grouped = true;
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        if (s + 16 * v < E) {
-          const float g = value_of(grp_row[((s + 16 * v) * inv_n) >> 16]);
-          if (near_keys(g, value_of(worst_in), width, slack) || near_keys(g, value_of(best_out), width, slack)) more |= 1 << v;
-        }
-    }
+    many = best_out != kNoKey && near_keys(value_of(worst_in), value_of(best_out), width, slack);
 #pragma unroll
     for (int v = 0; v < 4; ++v)
       if (!((open >> (((s + 16 * v) * inv_n) >> 16)) & 1)) key[v] = kNoKey;
   }
-  int first[4];
-#pragma unroll
-  for (int v = 0; v < 4; ++v) first[v] = key[v];
   // a lane's keys in descending order, their experts in the bytes of ex
   int ex = s | (s + 16) << 8 | (s + 32) << 16 | (s + 48) << 24;
   auto order = [&](int i, int j) __attribute__((always_inline)) {
@@ -212,44 +202,31 @@ __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_
     ex ^= x << (8 * i) | x << (8 * j);
   };
   order(0, 1); order(2, 3); order(0, 2); order(1, 3); order(1, 2);
-  float last = INFINITY;
-  int surplus = 0;   // keys taken less rounds: equal keys of several lanes go together, and are close
+  float last = INFINITY, before = INFINITY;
+  int surplus = 0, pair = 0;   // keys taken less rounds: equal keys of several lanes go together
 #pragma unroll 1
-  for (int j = 0; j <= a.k; ++j) {
+  for (int j = 0; j <= a.k + 1; ++j) {
     const int m = row_max(key[0]);
     const float mv = value_of(m);
     const bool some = m != kNoKey, hit = some && key[0] == m;
-    close |= some && j > 0 && near_keys(last, mv, 2.0f * delta, slack);
-    last = mv;
-    surplus += (hit ? 1 : 0) - (some && s == 0 ? 1 : 0);
-    if (hit && j < a.k) {
-      sel[j] = ex & 0xFF;
-      m_row[j] = m;
+    if (j <= a.k) {
+      const bool close = some && j > 0 && near_keys(last, mv, 2.0f * delta, slack);
+      many |= close && pair != 0;
+      pair = close ? j : pair;
+      surplus += (hit ? 1 : 0) - (some && s == 0 ? 1 : 0);
+      if (hit) sel[j] = ex & 0xFF;
+    } else {
+      many |= some && pair == a.k && near_keys(before, mv, 2.0f * delta, slack);   // a third one at the end of the selection
     }
+    before = last;
+    last = mv;
     key[0] = hit ? key[1] : key[0];
     key[1] = hit ? key[2] : key[1];
     key[2] = hit ? key[3] : key[2];
     key[3] = hit ? kNoKey : key[3];
     ex = hit ? ex >> 8 : ex;
   }
-  close |= row_sum(surplus) > 0;
-  if (__ballot(close)) {   // rare
-    wave_lds_fence();
-#pragma unroll 1
-    for (int j = 0; j < a.k; ++j) {   // experts whose key may lie on the other side of a selected one, itself included
-      const int m = m_row[j];
-      int count = 0, at = 0;
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        if (close && sel[j] >= 0 && first[v] != kNoKey && near_keys(value_of(first[v]), value_of(m), 2.0f * delta, slack)) {
-          ++count;
-          at |= 1 << v;
-        }
-      if (row_sum(count) > 1) more |= at;
-    }
-    if (grouped || row_sum(surplus) > 0) more |= 16;
-  }
-  return more;
+  return many || row_sum(surplus) > 0 ? -1 : pair;
 }
 
 // The same for one token by a whole wavefront (lane e: expert e), on fp64 keys: the rare case, compact rather than fast.
@@ -290,6 +267,8 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
     const double gs = a.group_top == 2 ? t1 + t2 : t1;
     grp_row[e] = gs;
     wave_lds_fence();
+    key_row[e] = a.group_top == 2 ? t2 : t1;   // the smallest key of the group's score
+    wave_lds_fence();
     int rank = 0;
 #pragma unroll 1
     for (int j = 0; j < G; ++j) {
@@ -300,8 +279,10 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
     const double worst_in = wave_min(e < G && rank < a.top_groups ? gs : INFINITY), best_out = wave_max(e < G && rank >= a.top_groups ? gs : kNone);
     const double mine = grp_row[min(e / n, G - 1)];
     const float w = width * static_cast<float>(a.group_top);
-    if (best_out > kNone && near_keys(worst_in, best_out, w, slack))   // the groups around the border
-      more |= __ballot(e < E && (near_keys(mine, worst_in, w, slack) || near_keys(mine, best_out, w, slack)));
+    const double least = key_row[min(e / n, G - 1)];
+    if (best_out > kNone && near_keys(worst_in, best_out, w, slack))   // what makes the scores of the groups around the border
+      more |= __ballot(key > kNone && (key > least || near_keys(key, least, width, slack)) &&
+                       (near_keys(mine, worst_in, w, slack) || near_keys(mine, best_out, w, slack)));
     if (e < E && !((open >> (e / n)) & 1)) key = kNone;
   }
   const double first = key;
@@ -330,18 +311,15 @@ struct RouteLds {
     double red[kRtWaves][32 * 64];                     // partial sums: the 32 (16) of a lane in stride
     struct {
       double key[kRtTokens][kRtRow], grp[kRtTokens][kRtRow];
-      int m[kRtTokens][8];
-      int pairs[kRtTokens * 64];                       // logits to settle: token << 6 | expert
-      double sum[kRtWaves][64], part[2][kRtWaves];
+      double sum[kRtWaves][64];
     } pick;
   };
   double l[kRtTokens][kRtRow];                 // finished logits
   float nx[kRtWaves][kRtTokens], nw[kRtWaves][128]; // shares of |x|^2 of the tokens and of |w|^2 of the experts (two each)
   uint32_t orx[kRtWaves][kRtTokens], orw[kRtWaves]; // bits of the values: all zero or not
   float x2[kRtTokens], w2;                     // |x|^2, the largest |w|^2; 0: nothing but zeros
-  int sel[kRtTokens][8];
+  int sel[kRtTokens][9];
   int cnt[64];
-  int n_pairs;
 };
 static_assert(sizeof(RouteLds) <= 160 * 1024, "LDS of a CU");
 
@@ -391,70 +369,51 @@ __global__ __launch_bounds__(256) void route_layout_kernel(const uint16_t* __res
   }
 }
 
-// fp64 logits of the listed pairs by the whole workgroup, two at a time (mostly the two of one token).  Code that a workgroup
-// in fifty reaches is fetched from memory when it does: here and below it is short rather than unrolled.
+// fp64 logits of two experts of a token by one wavefront, half of it for each.  Code that a workgroup in fifty reaches is fetched
+// from memory when it does (some 1000 cycles for 64 bytes of it, under the stream of the hidden states): here and below it
+// is short rather than unrolled.
 template <bool LAID>
-__device__ __forceinline__ void settle_logits(const RouteArgs& a, int t0, RouteLds& lds) {
-  const int tid = threadIdx.x, n = lds.n_pairs;
-#pragma unroll 1
-  for (int at = 0; at < n; at += 2) {
-    double s[2] = {0.0, 0.0};
-#pragma unroll 1
-    for (int c = 8 * tid; c < a.d; c += 8 * kRtThreads) {
-      u4 x[2], w[2];
+__device__ __forceinline__ void settle_two(const RouteArgs& a, int tok, int e0, int e1, double* l_row) {
+  const int lane = threadIdx.x & 63, e = lane < 32 ? e0 : e1;
+  const uint16_t* const xr = a.x + static_cast<int64_t>(tok) * a.d;
+  double s = 0.0;
+#pragma unroll 2
+  for (int c = 8 * (lane & 31); c < a.d; c += 8 * 32) {
+    const u4 x = *reinterpret_cast<const u4*>(xr + c);
+    u4 w;
+    if constexpr (LAID) {
+      w = a.cols[(static_cast<int64_t>(e) * a.d + c) >> 3];
+    } else {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int p = lds.pick.pairs[min(at + i, n - 1)], e = p & 63;
-        x[i] = *reinterpret_cast<const u4*>(a.x + static_cast<int64_t>(t0 + (p >> 6)) * a.d + c);
-        if constexpr (LAID) {
-          w[i] = a.cols[(static_cast<int64_t>(e) * a.d + c) >> 3];
-        } else {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            w[i][q] = a.w_router[static_cast<size_t>(c + 2 * q) * a.E + e] | static_cast<uint32_t>(a.w_router[static_cast<size_t>(c + 2 * q + 1) * a.E + e]) << 16;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          s[i] = fma(static_cast<double>(bf16_lo(x[i][q])), static_cast<double>(bf16_lo(w[i][q])), s[i]);
-          s[i] = fma(static_cast<double>(bf16_hi(x[i][q])), static_cast<double>(bf16_hi(w[i][q])), s[i]);
-        }
+      for (int q = 0; q < 4; ++q)
+        w[q] = a.w_router[static_cast<size_t>(c + 2 * q) * a.E + e] | static_cast<uint32_t>(a.w_router[static_cast<size_t>(c + 2 * q + 1) * a.E + e]) << 16;
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      s[i] = wave_add(s[i]);
-      if ((tid & 63) == 0) lds.pick.part[i][tid >> 6] = s[i];
+    for (int q = 0; q < 4; ++q) {   // fp64 products: of large values, beyond fp32, they are finite
+      s = fma(static_cast<double>(bf16_lo(x[q])), static_cast<double>(bf16_lo(w[q])), s);
+      s = fma(static_cast<double>(bf16_hi(x[q])), static_cast<double>(bf16_hi(w[q])), s);
     }
-    __syncthreads();
-    if (tid < 2 && at + tid < n) {
-      double sum = 0.0;
-#pragma unroll 1
-      for (int i = 0; i < kRtWaves; ++i) sum += lds.pick.part[tid][i];
-      const int p = lds.pick.pairs[at + tid];
-      lds.l[p >> 6][p & 63] = sum;
-    }
-    __syncthreads();
   }
+  s = row_sum(s);
+  s += __shfl_xor(s, 16, kWave);
+  if ((lane & 31) == 0) l_row[e] = s;
+  wave_lds_fence();
 }
 
-// Puts the two experts of a token that were too close into their order: e0 < e1, settled; lane 0 and lane 1 of the wavefront
-// have one each.  Both are selected or one of them is.  Keys are logits or sigmoid scores: softmax scores of a row have a
-// denominator, which takes route_select_exact.
-__device__ __forceinline__ void order_two(const RouteArgs& a, const double* l_row, int* sel, int e0, int e1) {
-  const int lane = threadIdx.x & 63, e = lane == 0 ? e0 : e1;
+// Puts the experts sel[j - 1] and sel[j], whose logits are settled, into their order; lanes 0 and 1 of the wavefront have one each.
+// Keys are logits or sigmoid scores: softmax scores of a row have a denominator, which takes route_select_exact.
+__device__ __forceinline__ void order_two(const RouteArgs& a, const double* l_row, int* sel, int j, int e0, int e1) {
+  const int e = (threadIdx.x & 63) == 0 ? e0 : e1;
   double key = l_row[e];
   if (!keys_are_logits(a)) {
     key = 1.0 / (1.0 + exp(-key));
     if (a.bias) key += static_cast<double>(a.bias[e]);
   }
   const double other = __shfl(key, 1, kWave);
-  const bool keep = __builtin_amdgcn_readlane(key >= other, 0);   // lane 0: e0 in front of e1
-  const int mine = lane < a.k ? sel[lane] : -1;
-  const uint64_t at = __ballot(mine == e0 || mine == e1);
-  const int win = keep ? e0 : e1, lose = keep ? e1 : e0;
-  if (at >> lane & 1) sel[lane] = (at & ((1ull << lane) - 1)) == 0 ? win : lose;
+  if ((threadIdx.x & 63) == 0 && !(key > other || (key == other && e0 < e1))) {
+    sel[j - 1] = e1;
+    sel[j] = e0;
+  }
 }
 
 // 64 channels of the 32 tokens and the router's rows of these channels: operands (LAID) or the rows as they lie in memory
@@ -483,7 +442,7 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
   // multiple of 4096 bytes, and so are the places of one memory channel)
   const int units = a.d / kRtUnit, u_begin = wave * units / kRtWaves, u_end = (wave + 1) * units / kRtWaves;
   if (tid < 64) lds.cnt[tid] = 0;
-  if (tid < kRtTokens * 8) lds.sel[tid >> 3][tid & 7] = -1;
+  if (tid < kRtTokens * 9) (&lds.sel[0][0])[tid] = -1;
 
   // 16-byte pieces of the tokens' units: eight lanes read the 128 bytes of a token, piece p of token t goes to place p ^ (t & 7) of
   // its 128 bytes of LDS, which spreads the operand reads (32 tokens, one piece) over the banks.  (Operands straight from memory
@@ -648,7 +607,6 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
     const int v = at >> 6, ln = at & 63;
     lds.l[(v & 3) + 8 * ((v >> 2) & 3) + 4 * (ln >> 5)][NF == 2 ? 2 * (ln & 31) + (v >> 4) : ln & 31] = sum;
   }
-  if (tid == 0) lds.n_pairs = 0;
   __syncthreads();
 
   // Selection: 16 lanes per token, all 32 at once.
@@ -657,68 +615,58 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
   const bool masked = live && a.mask != nullptr && a.mask[tok] == 0;
   // squares that underflow say nothing; products below the smallest normal value are off by an absolute amount
   const float x2 = lds.x2[t], w2 = lds.w2;
-  const bool zero = x2 == 0.0f || w2 == 0.0f;   // all logits are exactly zero
-  float tol = kRtBound * sqrtf(x2) * sqrtf(w2) + 0x1p-120f;
+  bool zero = x2 == 0.0f || w2 == 0.0f;   // all logits are exactly zero
+  float tol = logit_bound(units) * sqrtf(x2) * sqrtf(w2) + 0x1p-120f;
   if (!(x2 > 0x1p-80f && w2 > 0x1p-80f)) tol = INFINITY;
   if (zero) tol = 0.0f;
   const bool vague = !(tol < INFINITY);   // the bound says nothing: every logit of the token is settled
   float sc[4], total;
   double shift;
   route_scores(a, lds.l[t], sc, shift, total);
-  int again = route_select(a, lds.l[t], sc, shift, reinterpret_cast<int*>(lds.pick.key[t]), reinterpret_cast<int*>(lds.pick.grp[t]), lds.pick.m[t],
-                           lds.sel[t], tol);
-  if (vague) {
-    again = 16;
-#pragma unroll
-    for (int v = 0; v < 4; ++v) again |= s + 16 * v < a.E ? 1 << v : 0;
-  }
-  if (!live || masked) again = 0;
-  // Rare: the logits that a selection hangs on are settled, and it is made again in fp64, until it hangs on none.
-  uint64_t b[5];
-#pragma unroll
-  for (int v = 0; v < 5; ++v) b[v] = __ballot(again >> v & 1);
-  const bool redo = (b[0] | b[1] | b[2] | b[3]) != 0;
-  if (__syncthreads_or(redo)) {
+  int state = route_select(a, lds.l[t], sc, shift, reinterpret_cast<int*>(lds.pick.key[t]), reinterpret_cast<int*>(lds.pick.grp[t]), lds.sel[t], tol);
+  if (vague || (state > 0 && (zero || !(a.sigmoid || keys_are_logits(a))))) state = -1;
+  if (!live || masked) state = 0;
+  // Rare: the logits that a selection hangs on are settled by the token's wavefront.  Two experts are put in order; otherwise the
+  // selection is made again in fp64 until it hangs on no logit that is not settled.
+  if (__ballot(state != 0)) {
+    wave_lds_fence();
     const uint64_t all = ~0ull >> (64 - a.E);
-    uint64_t exact[4];
-    const bool pairs_do = a.sigmoid || keys_are_logits(a);
-    int todo = 0, two = 0;   // tokens of this wavefront; those with two experts to put in order
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      uint64_t m = 0;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) m |= ((b[v] >> (16 * q)) & 0xFFFFull) << (16 * v);
-      todo |= m ? 1 << q : 0;
-      if (pairs_do && __builtin_popcountll(m) == 2 && !((b[4] >> (16 * q)) & 0xFFFF) && !__builtin_amdgcn_readlane(zero, 16 * q)) two |= 1 << q;
-      exact[q] = __builtin_amdgcn_readlane(zero, 16 * q) ? all : m;
-      if (exact[q] == m && (m >> lane & 1)) lds.pick.pairs[atomicAdd(&lds.n_pairs, 1)] = (4 * wave + q) << 6 | lane;
-    }
-    for (;;) {
-      if (!__syncthreads_or(todo)) break;
-      settle_logits<LAID>(a, t0, lds);
-      __syncthreads();
-      if (tid == 0) lds.n_pairs = 0;
-      __syncthreads();
 #pragma unroll 1
-      for (int q = 0; q < 4; ++q) {
-        if (!(todo >> q & 1)) continue;
-        const int tq = 4 * wave + q;
-        const float tol_q = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(tol), 16 * q));
-        const uint64_t done = q == 0 ? exact[0] : q == 1 ? exact[1] : q == 2 ? exact[2] : exact[3];
-        if (two >> q & 1) {
-          order_two(a, lds.l[tq], lds.sel[tq], __builtin_ctzll(done), 63 - __builtin_clzll(done));
-          todo &= ~(1 << q);
-          continue;
+    for (int q = 0; q < 4; ++q) {
+      const int st = __builtin_amdgcn_readlane(state, 0);
+      const bool z = __builtin_amdgcn_readlane(zero, 0);
+      const float tol_q = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(tol), 0));
+      // the next row of lanes takes the place of the first
+      state = __shfl(state, lane + 16, kWave);
+      tol = __shfl(tol, lane + 16, kWave);
+      zero = __shfl(static_cast<int>(zero), lane + 16, kWave) != 0;
+      if (st == 0) continue;
+      const int tq = 4 * wave + q;
+      double* const l_row = lds.l[tq];
+      int* const sel = lds.sel[tq];
+      if (st > 0) {
+        const int e0 = __builtin_amdgcn_readfirstlane(sel[st - 1]), e1 = __builtin_amdgcn_readfirstlane(sel[st]);
+        settle_two<LAID>(a, t0 + tq, e0, e1, l_row);
+        order_two(a, l_row, sel, st, e0, e1);
+        continue;
+      }
+      uint64_t exact = z ? all : 0, next = tol_q < INFINITY ? 0 : all;
+      for (;;) {
+        exact |= next;
+#pragma unroll 1
+        while (next) {
+          const int e0 = __builtin_ctzll(next);
+          next &= next - 1;
+          const int e1 = next ? __builtin_ctzll(next) : e0;
+          if (next) next &= next - 1;
+          settle_two<LAID>(a, t0 + tq, e0, e1, l_row);
         }
-        const uint64_t next = route_select_exact(a, lds.l[tq], lds.pick.key[tq], lds.pick.grp[tq], lds.sel[tq], tol_q, done);
-        if (next == 0) todo &= ~(1 << q);
-        if (next >> lane & 1) lds.pick.pairs[atomicAdd(&lds.n_pairs, 1)] = tq << 6 | lane;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i == q) exact[i] |= next;
+        next = route_select_exact(a, l_row, lds.pick.key[tq], lds.pick.grp[tq], sel, tol_q, exact);
+        if (next == 0) break;
       }
     }
-    if (redo) route_scores(a, lds.l[t], sc, shift, total);
+    wave_lds_fence();
+    route_scores(a, lds.l[t], sc, shift, total);
   }
   wave_lds_fence();
   // weights: lane j < k has slot j
