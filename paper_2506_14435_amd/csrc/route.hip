@@ -327,45 +327,50 @@ static_assert(sizeof(RouteLds) <= 160 * 1024, "LDS of a CU");
 // bytes, lane 32 g + r: channels 16 s + 8 g .. + 7 of expert r (NF = 1, E <= 32) or 2 r + f (NF = 2).  And as columns [E, d],
 // for logits that are settled (reading them out of the operands, a line of memory for 16 bytes, took 13000 cycles for two).
 // One unit per workgroup, which also leaves every expert's share of |w|^2 and the bits of its values.
+constexpr int kLayThreads = 1024;   // four elements and one or two pieces a thread: the kernel is a chain of latencies
 template <int NF>
-__global__ __launch_bounds__(256) void route_layout_kernel(const uint16_t* __restrict__ w, int d, int E, u4* __restrict__ ops, u4* __restrict__ cols,
-                                                           float* __restrict__ w2, uint32_t* __restrict__ bits) {
+__global__ __launch_bounds__(kLayThreads) void route_layout_kernel(const uint16_t* __restrict__ w, int d, int E, u4* __restrict__ ops, u4* __restrict__ cols,
+                                                                   float* __restrict__ w2, uint32_t* __restrict__ bits) {
   __shared__ uint16_t s_w[kRtUnit][64 + 2];
-  __shared__ float s_n[4][64];
-  __shared__ uint32_t s_any[4][64];
+  __shared__ float s_n[16][64];
+  __shared__ uint32_t s_any[16][64];
   const int u = blockIdx.x, tid = threadIdx.x, e = tid & 63, part = tid >> 6;
   const uint16_t* const src = w + static_cast<int64_t>(u) * kRtUnit * E;
-  uint16_t v[16];
+  uint16_t v[4];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = e < E ? src[(16 * part + i) * E + e] : 0;
+  for (int i = 0; i < 4; ++i) v[i] = e < E ? src[(4 * part + i) * E + e] : 0;
   float n = 0.0f;
   uint32_t any = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    s_w[16 * part + i][e] = v[i];
+  for (int i = 0; i < 4; ++i) {
+    s_w[4 * part + i][e] = v[i];
     n = fmaf(bf16_to_f32(v[i]), bf16_to_f32(v[i]), n);
     any |= v[i] & 0x7FFFu;
   }
   s_n[part][e] = n;
   s_any[part][e] = any;
   __syncthreads();
-  auto piece = [&](int c, int col) {   // channels c .. c + 7 of an expert
+  // the lower threads write the operands, the upper ones the columns: eight channels of an expert each
+  const bool op = tid < 512;
+  const int i = tid & 511, lane = i & 63, f = (i >> 6) % NF, s = (i >> 6) / NF;
+  const int c = op ? 16 * s + 8 * (lane >> 5) : 8 * (i & 7), col = op ? (NF == 2 ? 2 * (lane & 31) + f : lane & 31) : i >> 3;
+  if (op ? i < 4 * NF * 64 : col < E) {
     u4 o;
 #pragma unroll
     for (int q = 0; q < 4; ++q) o[q] = s_w[c + 2 * q][col] | static_cast<uint32_t>(s_w[c + 2 * q + 1][col]) << 16;
-    return o;
-  };
-#pragma unroll
-  for (int i = tid; i < 4 * NF * 64; i += 256) {
-    const int lane = i & 63, f = (i >> 6) % NF, s = (i >> 6) / NF;
-    ops[static_cast<int64_t>(u) * 4 * NF * 64 + i] = piece(16 * s + 8 * (lane >> 5), NF == 2 ? 2 * (lane & 31) + f : lane & 31);
+    if (op) ops[static_cast<int64_t>(u) * 4 * NF * 64 + i] = o;
+    else cols[static_cast<int64_t>(col) * (d >> 3) + u * 8 + (i & 7)] = o;
   }
+  if (part == 0) {
+    n = 0.0f;
+    any = 0;
 #pragma unroll
-  for (int i = tid; i < 8 * 64; i += 256)
-    if (i >> 3 < E) cols[static_cast<int64_t>(i >> 3) * (d >> 3) + u * 8 + (i & 7)] = piece(8 * (i & 7), i >> 3);
-  if (tid < 64) {
-    w2[u * 64 + tid] = (s_n[0][tid] + s_n[1][tid]) + (s_n[2][tid] + s_n[3][tid]);
-    bits[u * 64 + tid] = s_any[0][tid] | s_any[1][tid] | s_any[2][tid] | s_any[3][tid];
+    for (int q = 0; q < 16; ++q) {
+      n += s_n[q][e];
+      any |= s_any[q][e];
+    }
+    w2[u * 64 + e] = n;
+    bits[u * 64 + e] = any;
   }
 }
 
@@ -776,10 +781,10 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
     a.op_w2 = w2;
     a.op_bits = bits;
     if (nf == 1) {
-      route_layout_kernel<1><<<units, 256, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
+      route_layout_kernel<1><<<units, kLayThreads, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
       route_kernel<1, true, 4, true><<<blocks, kRtThreads, 0, stream>>>(a);
     } else {
-      route_layout_kernel<2><<<units, 256, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
+      route_layout_kernel<2><<<units, kLayThreads, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
       route_kernel<2, true, 8, true><<<blocks, kRtThreads, 0, stream>>>(a);
     }
   } else if (a.T > 0) {
