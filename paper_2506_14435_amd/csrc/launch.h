@@ -238,10 +238,11 @@ struct RouteBackwardArgs {
   float scale;
   float* dx;                  // or null
   float* dw;                  // or null
-  // workspace: dlogits as operands of both products, the weights as operands of dx, shares of dw
+  // workspace: dlogits as operands of both products, the weights as operands of dx, the tokens that take part, shares of dw
   unsigned int __attribute__((ext_vector_type(4)))* ga;
   unsigned int __attribute__((ext_vector_type(4)))* gb;
   unsigned int __attribute__((ext_vector_type(4)))* wa;
+  uint32_t* keep;
   float* dw_part;
 };
 size_t route_backward_workspace_bytes(int T, int d, int E);

@@ -828,7 +828,7 @@ mote_status mote_route_backward(const mote_routing* cfg, const void* x, const vo
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOTE_ERR_INVALID_ARG;
   if (workspace_bytes < route_backward_workspace_bytes(T, d, E)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
   RouteBackwardArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_router), logits, topk_idx, d_topk_w, d_score_sum, token_mask,
-                      T, d, E, cfg->top_k, cfg->score == MOTE_SCORE_SIGMOID, cfg->renormalise != 0, cfg->scale, dx, dw_router, nullptr, nullptr, nullptr, nullptr};
+                      T, d, E, cfg->top_k, cfg->score == MOTE_SCORE_SIGMOID, cfg->renormalise != 0, cfg->scale, dx, dw_router, nullptr, nullptr, nullptr, nullptr, nullptr};
   MOTE_HIP(launch_route_backward(a, workspace, static_cast<hipStream_t>(hip_stream)));
   return MOTE_OK;
 }

@@ -846,7 +846,7 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
   if (a.sigmoid) {
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      const float t = expf(-fabsf(l[v])), r = 1.0f / (1.0f + t);
+      const float t = exp_of(-fabsf(l[v])), r = __builtin_amdgcn_rcpf(1.0f + t);
       sc[v] = l[v] >= 0.0f ? r : t * r;
       om[v] = l[v] >= 0.0f ? t * r : r;   // 1 - s
     }
@@ -855,7 +855,7 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
     float sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      sc[v] = s + 16 * v < E ? expf(l[v] - mx) : 0.0f;
+      sc[v] = s + 16 * v < E ? exp_of(l[v] - mx) : 0.0f;
       om[v] = 1.0f;
       sum += sc[v];
     }
@@ -868,14 +868,14 @@ __device__ __forceinline__ void route_grad_token(const RouteBackwardArgs& a, int
     float al[4], m = -INFINITY;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      al[v] = a.sigmoid ? fminf(l[v], 0.0f) - log1pf(expf(-fabsf(l[v]))) : l[v];
+      al[v] = a.sigmoid ? fminf(l[v], 0.0f) - 0.69314718f * __builtin_amdgcn_logf(1.0f + exp_of(-fabsf(l[v]))) : l[v];
       if (sel[v] > 0.0f) m = fmaxf(m, al[v]);
     }
     m = row_max(m);
     float p[4], sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      p[v] = sel[v] > 0.0f ? expf(al[v] - m) : 0.0f;
+      p[v] = sel[v] > 0.0f ? exp_of(al[v] - m) : 0.0f;
       sum += p[v] * sel[v];
     }
     sum = row_sum(sum);
@@ -938,7 +938,7 @@ __device__ __forceinline__ void three_terms(float g, uint32_t (&t)[3]) {
 template <int NS, int NT>
 __global__ __launch_bounds__(512) void route_dlogits_kernel(RouteBackwardArgs a) {
   __shared__ float s_g[32][65];
-  __shared__ int s_e[32][8];
+  __shared__ int s_e[32][8], s_keep[32];
   __shared__ float s_d[32][8];
   const int tid = threadIdx.x, tiles = (a.T + 31) / 32;
   if (static_cast<int>(blockIdx.x) >= tiles) {
@@ -961,7 +961,12 @@ __global__ __launch_bounds__(512) void route_dlogits_kernel(RouteBackwardArgs a)
   route_grad_token(a, min(tok, a.T - 1), tok < a.T, s_e[t], s_d[t], g);
 #pragma unroll
   for (int v = 0; v < 4; ++v) s_g[t][s + 16 * v] = g[v];
+  if (s == 0) s_keep[t] = tok < a.T && (a.mask == nullptr || a.mask[tok] != 0);
   __syncthreads();
+  if (tid < 64) {   // a bit for every token that takes part, 16 in a word
+    const uint32_t b = static_cast<uint32_t>(__ballot(tid < 32 && s_keep[tid & 31] != 0));
+    if (tid < 2) a.keep[blockIdx.x * 2 + tid] = (b >> (16 * tid)) & 0xFFFFu;
+  }
 #pragma unroll 1
   for (int i = tid; i < (NS + 2 * NT) * 64; i += 512) {
     const bool first = i < NS * 64;
@@ -1062,8 +1067,7 @@ __global__ __launch_bounds__(64 * kDwWaves) void route_dw_kernel(RouteBackwardAr
         for (int v = 0; v < 16; ++v) acc[j][o][n][v] = 0.0f;
   struct Step {
     u4 x[4], g[3][NT];
-    uint32_t keep[4];   // 0: a padding token, which has no part whatever its row holds
-    int s;
+    uint32_t keep;   // a padding token has no part, whatever its row holds
   };
   auto load = [&](int s) __attribute__((always_inline)) {
     Step q;
@@ -1073,9 +1077,8 @@ __global__ __launch_bounds__(64 * kDwWaves) void route_dw_kernel(RouteBackwardAr
       const int t = 16 * s + 4 * i + (lane >> 4);
       const uint16_t* const row = a.x + static_cast<int64_t>(min(t, a.T - 1)) * a.d + c0 + 8 * (lane & 15);
       q.x[i] = *reinterpret_cast<const u4*>(row);
-      q.keep[i] = a.mask != nullptr ? a.mask[min(t, a.T - 1)] : 1u;
     }
-    q.s = s;
+    q.keep = load_uniform(a.keep + s);
 #pragma unroll
     for (int p = 0; p < 3; ++p)
 #pragma unroll
@@ -1087,7 +1090,7 @@ __global__ __launch_bounds__(64 * kDwWaves) void route_dw_kernel(RouteBackwardAr
   auto compute = [&](const Step& q) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const bool in = q.keep[i] != 0 && 16 * q.s + 4 * i + (lane >> 4) < a.T;
+      const bool in = (q.keep >> (4 * i + (lane >> 4))) & 1;
       *reinterpret_cast<u4*>(stage + 1024 * i + 16 * lane) = in ? q.x[i] : u4{0u, 0u, 0u, 0u};
     }
     wave_lds_fence();
@@ -1190,7 +1193,7 @@ int dw_shares(int T, int d) {
   return std::max(std::min(want, most), 1);
 }
 struct BackwardLayout {
-  size_t ga, gb, wa, part, bytes;
+  size_t ga, gb, wa, keep, part, bytes;
 };
 BackwardLayout backward_layout(int T, int d, int E) {
   const size_t tiles = (static_cast<size_t>(T) + 31) / 32, ns = steps_of(E), nt = E <= 32 ? 1 : 2;
@@ -1200,6 +1203,7 @@ BackwardLayout backward_layout(int T, int d, int E) {
   l.ga = take(tiles * 3 * ns * 1024);
   l.gb = take(tiles * 2 * 3 * nt * 1024);
   l.wa = take(static_cast<size_t>(d / 32) * ns * 1024);
+  l.keep = take(tiles * 2 * sizeof(uint32_t));
   l.part = take(dw_shares(T, d) > 1 ? static_cast<size_t>(dw_shares(T, d)) * d * 32 * nt * sizeof(float) : 0);
   l.bytes = std::max<size_t>(at, 256);
   return l;
@@ -1219,6 +1223,7 @@ hipError_t launch_route_backward(RouteBackwardArgs a, void* workspace, hipStream
   a.ga = reinterpret_cast<u4*>(ws + l.ga);
   a.gb = reinterpret_cast<u4*>(ws + l.gb);
   a.wa = reinterpret_cast<u4*>(ws + l.wa);
+  a.keep = reinterpret_cast<uint32_t*>(ws + l.keep);
   a.dw_part = reinterpret_cast<float*>(ws + l.part);
   const unsigned lay = static_cast<unsigned>((a.T + 31) / 32 + a.d / 32);
   int slice = 256;
