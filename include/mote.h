@@ -187,7 +187,8 @@ mote_status mote_router_balance(const void* x, const void* w_router, const float
  * The selection bias decides who is selected and has no part in the weights.  An expert whose key is -inf (a bias of -inf
  * switches it off) is never selected: slots that find no expert get index -1 and weight 0.  A NaN key ranks as the lowest
  * finite value: indices stay in range and the weights carry the NaN.  Indices follow from fp64 logits whatever kernel
- * computes them: sums whose order could matter are settled in fp64 before an index is written.
+ * computes them: sums whose rounding could matter are settled in fp64 before an index is written (keys of different columns
+ * that fp64 itself rounds together may fall either way; equal columns go to the lower index).
  *
  * cfg          in : the description above; top_k <= 8 and at most the experts of top_groups groups, n_groups divides E,
  *                   group_top 1 or 2 and at most E / n_groups.  n_groups == 1: no groups (top_groups, group_top 1)
@@ -196,7 +197,7 @@ mote_status mote_router_balance(const void* x, const void* w_router, const float
  * token_mask   in : uint8 [T] or NULL; a token whose byte is 0 is padding: indices -1, weights 0, not counted, not in
  *                   the score sums
  * topk_idx     out: int32 [T, top_k];   topk_w out: fp32 [T, top_k]
- * logits       out: fp32 [T, E] or NULL (mote_route_backward reads them; written for padding too)
+ * logits       out: fp32 [T, E] or NULL (mote_route_backward reads them, but not those of padding)
  * expert_counts out: int32 [E] or NULL; number of (token, slot) pairs of each expert
  * score_sum    out: fp32 [E] or NULL; sum over the tokens of s (fp64 sums in a fixed order): with expert_counts the two
  *                   factors of Eq.12

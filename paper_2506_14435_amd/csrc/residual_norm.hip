@@ -208,9 +208,11 @@ __global__ __launch_bounds__(block_threads<NT>()) void residual_norm_backward_ke
     const bool store = in && row < a.T;
     const int64_t at = row * a.d + c;
     float hat_y[8] = {}, z[8], up[8] = {}, hat[8] = {}, dn[8] = {}, inv_y = 1.0f;
-    if (store) {   // a row behind the last is zeros: nothing of it reaches a sum
+    if (in) {
       raw.y.get(hat_y);
       raw.r.get(hat);
+    }
+    if (store) {   // behind the last row it is that row once more, with zero gradients: nothing of it reaches a sum
       if (d_normed != nullptr) raw.n.get(dn);
       if (d_total != nullptr) raw.t.get(up);
     }
