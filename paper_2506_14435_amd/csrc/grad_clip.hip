@@ -121,9 +121,9 @@ __global__ __launch_bounds__(kThreads) void grad_square_kernel(const Table t, do
   if (threadIdx.x == 0) partial[blockIdx.x] = acc;
 }
 
-// c == 1: a copy, bits as they are.  stream: the stores go past the caches.
+// c == 1: a copy, bits as they are
 template <typename T>
-__device__ __forceinline__ void scale_unit(const T* g, T* o, int n, bool clip, double c, bool stream) {
+__device__ __forceinline__ void scale_unit(const T* g, T* o, int n, bool clip, double c) {
   constexpr int N = Vec<T>::N, V = kPart / N / kThreads;
   if ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(o)) % 16 == 0) {
     const u4* const p = reinterpret_cast<const u4*>(g);
@@ -134,11 +134,7 @@ __device__ __forceinline__ void scale_unit(const T* g, T* o, int n, bool clip, d
       if ((i * kThreads + static_cast<int>(threadIdx.x) + 1) * N <= n) v[i] = p[i * kThreads + threadIdx.x];
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if ((i * kThreads + static_cast<int>(threadIdx.x) + 1) * N <= n) {
-        const u4 s = clip ? Vec<T>::scaled(v[i], c) : v[i];
-        if (stream) __builtin_nontemporal_store(s, q + i * kThreads + threadIdx.x);
-        else q[i * kThreads + threadIdx.x] = s;
-      }
+      if ((i * kThreads + static_cast<int>(threadIdx.x) + 1) * N <= n) q[i * kThreads + threadIdx.x] = clip ? Vec<T>::scaled(v[i], c) : v[i];
     const int rest = n / N * N + threadIdx.x;
     if (rest < n) o[rest] = clip ? Vec<T>::scaled_one(g[rest], c) : g[rest];
   } else {
@@ -148,7 +144,7 @@ __device__ __forceinline__ void scale_unit(const T* g, T* o, int n, bool clip, d
 
 // Units from the last to the first: what the kernel before read last is still in the memory-side cache.
 __global__ __launch_bounds__(kThreads) void grad_scale_kernel(const Table t, const double* __restrict__ partial, int partials, float max_norm,
-                                                              bool stream, float* __restrict__ norm_out) {
+                                                              float* __restrict__ norm_out) {
   __shared__ double s[4];
   double acc = 0.0;
 #pragma unroll 4
@@ -170,8 +166,8 @@ __global__ __launch_bounds__(kThreads) void grad_scale_kernel(const Table t, con
 #pragma unroll 1
     for (int h = 0; h < n; h += kPart) {
       const int m = min(n - h, kPart);
-      if (bf16) scale_unit(static_cast<const uint16_t*>(t.grad[i]) + at + h, static_cast<uint16_t*>(t.out[i]) + at + h, m, clip, c, stream);
-      else scale_unit(static_cast<const float*>(t.grad[i]) + at + h, static_cast<float*>(t.out[i]) + at + h, m, clip, c, stream);
+      if (bf16) scale_unit(static_cast<const uint16_t*>(t.grad[i]) + at + h, static_cast<uint16_t*>(t.out[i]) + at + h, m, clip, c);
+      else scale_unit(static_cast<const float*>(t.grad[i]) + at + h, static_cast<float*>(t.out[i]) + at + h, m, clip, c);
     }
   }
 }
@@ -199,16 +195,11 @@ void fill(const GradTensor* g, int at, int n, Table* t) {
 
 size_t grad_clip_workspace_bytes(int n) { return 256 + static_cast<size_t>(n / kTable + 2) * kSquareBlocks * sizeof(double); }
 
-// Lists beyond this many units (32 KB of fp32 each): results are stored past the caches, which cannot hold them and keep gradients
-// instead.  118 M elements, norm + scaling: 107 + 154 us without, 78 to 92 + 152 with (the first pass finds a part of what the call
-// before left there; reading past the caches as well 67 + 166).  Smaller lists fit, and what comes next finds the results there.
-constexpr int kStreamUnits = 4800;
-
+// Results are stored through the caches, where the optimiser finds the last of them.  (Past the caches the scaling takes the same
+// time, 118 M elements 154 and 152 us.  A first pass over the gradients of the call before would find more of them, 92 us instead of
+// 107; a training step has new ones.)
 hipError_t launch_grad_clip(const GradTensor* g, int n, float max_norm, float* norm, void* workspace, hipStream_t stream) {
   double* const partial = static_cast<double*>(workspace);
-  int64_t units = 0;
-  for (int i = 0; i < n; ++i) units += (g[i].n + kUnit - 1) / kUnit;
-  const bool past = units > kStreamUnits;
   int partials = 0;
   Table t{};
   for (int at = 0; at < n; at += kTable) {
@@ -220,7 +211,7 @@ hipError_t launch_grad_clip(const GradTensor* g, int n, float max_norm, float* n
   for (int at = n > 0 ? (n - 1) / kTable * kTable : 0; at >= 0; at -= kTable) {
     fill(g, at, n, &t);
     const int blocks = std::max(std::min(t.first[t.count], kScaleBlocks), 1);
-    grad_scale_kernel<<<blocks, kThreads, 0, stream>>>(t, partial, partials, max_norm, past, norm);
+    grad_scale_kernel<<<blocks, kThreads, 0, stream>>>(t, partial, partials, max_norm, norm);
   }
   return hipGetLastError();
 }
