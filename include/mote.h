@@ -228,7 +228,7 @@ mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_rou
  *
  * d_score_sum of Eq.12 with weight gamma is gamma * E / T * expert_counts (counts are constants there too).
  * Operands of the two products are exact (fp32 dlogits as three bf16 terms against bf16 x and w_router), sums are fp32 in a
- * fixed order.  A padding token (token_mask) has a zero gradient row; slots of index -1 have no part.
+ * fixed order.  A padding token (token_mask) has a zero gradient row (finite w_router); slots of index -1 have no part.
  *
  * cfg: score, top_k, renormalise and scale as in the forward call (groups and bias do not enter)
  * logits in : fp32 [T, E] of the forward call;  topk_idx in : int32 [T, top_k];  d_topk_w in : fp32 [T, top_k]
@@ -363,7 +363,8 @@ mote_status mote_layer_forward_routed(const mote_layer* layer, const void* x, in
  * N is the norm of mote_block_forward.  Everything between the loads and the two stores is fp32 (row sums included); normed
  * is taken from the sum before its rounding.
  * dtype        : MOTE_DTYPE_BF16 or MOTE_DTYPE_F32, of r, y, total, normed and their gradients; gamma, beta, gate: bf16 [d]
- * r, y     in  : [T, d];   total, normed out : [T, d]
+ * r, y     in  : [T, d];   total, normed out : [T, d]; each may be r or y itself (a row is loaded
+ *                   before it is stored), not both the same one
  * Limits: d % 8 == 0, 8 <= d <= 8192; eps >= 0, scales finite.  T == 0 is a no-op. */
 typedef struct {
   const mote_norm* post;

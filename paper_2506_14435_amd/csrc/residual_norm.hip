@@ -116,9 +116,9 @@ __device__ __forceinline__ float normalise(RowSum<NT>& sum, int kind, float eps,
   return inv;
 }
 
+// total and normed may be r or y
 template <int NT, typename T>
-__global__ __launch_bounds__(block_threads<NT>()) void residual_norm_kernel(ResidualArgs a, const T* __restrict__ r, const T* __restrict__ y,
-                                                                            T* __restrict__ total, T* __restrict__ normed) {
+__global__ __launch_bounds__(block_threads<NT>()) void residual_norm_kernel(ResidualArgs a, const T* r, const T* y, T* total, T* normed) {
   constexpr int kRows = rows_of_block<NT>();
   __shared__ float s_buf[kRows][2 * (NT / 64)][2];
   const int slot = threadIdx.x / NT, c = (threadIdx.x % NT) * 8;
@@ -344,7 +344,7 @@ int threads_of_row(int d) {
 int backward_blocks(int T, int d, bool f32) {
   const int nt = threads_of_row(d), rows = std::max(256 / nt, 1);
   const int most = std::max((f32 ? 512 : 768) * 256 / std::max(nt, 256), 256);
-  return std::max(std::min((T + 2 * rows - 1) / (2 * rows), most), 1);
+  return static_cast<int>(std::max<int64_t>(std::min<int64_t>((static_cast<int64_t>(T) + 2 * rows - 1) / (2 * rows), most), 1));
 }
 
 template <int NT, typename T>

@@ -479,6 +479,23 @@ def test_residual_writes_nothing_behind_the_last_row():
         assert all((b[T:] == 7.0).all() and (b[:T] != 7.0).any() for b in buf)
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,d", [(1, 8), (37, 264), (5000, 1032), (3, 8192)])
+def test_residual_in_place(T, d, dt):
+    """Outputs in the place of the inputs: the same bits as in memory of their own."""
+    g = torch.Generator().manual_seed(T + d)
+    block, _ = _block(d, "layer", "rms", True, g)
+    r, y = torch.randn(T, d, generator=g).cuda().to(dt), torch.randn(T, d, generator=g).cuda().to(dt)
+    want = M.mote_residual_norm(block, r, y)
+    for into_r in (True, False):
+        r2, y2 = r.clone(), y.clone()
+        total, normed = (r2, y2) if into_r else (y2, r2)
+        got = M.mote_residual_norm(block, r2, y2, total=total, normed=normed)
+        torch.cuda.synchronize()
+        assert got[0] is total and got[1] is normed
+        assert torch.equal(total, want[0]) and torch.equal(normed, want[1]), into_r
+
+
 def test_residual_norm_of_no_rows():
     g = torch.Generator().manual_seed(9)
     block, _ = _block(256, "rms", "layer", True, g)
