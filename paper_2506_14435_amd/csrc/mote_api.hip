@@ -785,7 +785,7 @@ mote_status mote_ste_linear_backward(const void* dy, const int32_t* offsets_host
 }
 
 size_t mote_route_workspace_bytes(int T, int d, int E) {
-  if (T < 0 || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
+  if (T < 0 || T >= (1 << 24) || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
   return route_workspace_bytes(T, d, E, true);
 }
 
@@ -813,7 +813,7 @@ mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_rou
 }
 
 size_t mote_route_backward_workspace_bytes(int T, int d, int E) {
-  if (T < 0 || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
+  if (T < 0 || T >= (1 << 24) || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
   return route_backward_workspace_bytes(T, d, E);
 }
 

@@ -202,6 +202,18 @@ def test_clip_refuses_on_the_host(lib):
     assert lib.mote_clip_grad_norm_workspace_bytes(-1) == 0 and lib.mote_clip_grad_norm_workspace_bytes(4097) == 0
 
 
+def test_workspace_sizes_at_the_ends_of_the_range(lib):
+    """Token counts that the calls refuse have no workspace; sizes do not fall as the count grows to the largest."""
+    for f in (lib.mote_route_workspace_bytes, lib.mote_route_backward_workspace_bytes):
+        for T in (1 << 24, (1 << 31) - 600, (1 << 31) - 1):
+            assert f(T, 256, 8) == 0, T
+        sizes = [f(T, 256, 8) for T in (1, 64, 65, 5000, 1 << 20, (1 << 24) - 1)]
+        assert sizes == sorted(sizes) and sizes[-1] > 0
+    block = ctypes.byref(B.MoteResidualStruct(None, None, 1.0, 1.0, _norm()))
+    sizes = [lib.mote_residual_norm_workspace_bytes(block, T, 8) for T in (1, 1000, 1 << 20, (1 << 31) - 1)]
+    assert sizes == sorted(sizes)
+
+
 def test_overlap_check_allows_what_does_not_overlap(lib):
     """Gradients that are only read may share memory, neighbours may touch.  The workspace is checked last: a list that passes
     ends there, before any launch."""
