@@ -727,3 +727,53 @@ def test_binding_refuses_shapes_types_and_strides():
             f()
             print("call", i, "went through")
     torch.cuda.synchronize()
+
+
+# ------------------------------------------------------------------------------------------- offsets beyond 32 bits
+def test_routing_of_more_than_2_31_elements():
+    """The last tokens of a batch whose rows pass 2^31 elements: the same bits as in a batch of their own that starts at a
+    multiple of 32 tokens; one token with a gradient gives dw in both (zeros change no sum)."""
+    T, d, E, tail = 32896, 65536, 8, 96
+    g = torch.Generator(device="cuda").manual_seed(40)
+    x = torch.randn(T, d, generator=g, device="cuda", dtype=torch.bfloat16)
+    w = (torch.randn(d, E, generator=g, device="cuda") * d ** -0.5).bfloat16()
+    last = x[-tail:].clone()
+    assert x[:-tail].numel() > 2 ** 31
+    cfg = M.MoteRouting(2, renormalise=True)
+    a, b = M.mote_route(x, w, cfg, want_logits=True, want_stats=True), M.mote_route(last, w, cfg, want_logits=True)
+    assert torch.equal(a.topk_idx[-tail:], b.topk_idx) and torch.equal(a.topk_w[-tail:], b.topk_w) and torch.equal(a.logits[-tail:], b.logits)
+    assert int(a.counts.sum()) == 2 * T
+    d_w = torch.zeros(T, 2, device="cuda")
+    d_w[-1] = torch.tensor([0.75, -0.5], device="cuda")
+    dx, dw = M.mote_route_backward(x, w, cfg, a.logits, a.topk_idx, d_w)
+    dx_b, dw_b = M.mote_route_backward(last, w, cfg, b.logits, b.topk_idx, d_w[-tail:].clone())
+    torch.cuda.synchronize()
+    assert torch.equal(dx[-tail:], dx_b) and (dx_b[-1] != 0).any() and not (dx[:8] != 0).any()
+    assert torch.equal(dw, dw_b) and (dw_b != 0).any()
+
+
+def test_residual_of_more_than_2_31_elements():
+    T, d, tail = 262400, 8192, 200
+    g = torch.Generator().manual_seed(41)
+    block, _ = _block(d, "rms", "layer", True, g)
+    gpu = torch.Generator(device="cuda").manual_seed(42)
+    r, y = (torch.randn(T, d, generator=gpu, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    assert r[:-tail].numel() > 2 ** 31
+    total, normed = M.mote_residual_norm(block, r, y)
+    want = M.mote_residual_norm(block, r[-tail:].clone(), y[-tail:].clone())
+    assert torch.equal(total[-tail:], want[0]) and torch.equal(normed[-tail:], want[1])
+    back = M.mote_residual_norm_backward(block, r, y, total, normed, want_params=False)
+    want = M.mote_residual_norm_backward(block, r[-tail:].clone(), y[-tail:].clone(), want[0], want[1], want_params=False)
+    torch.cuda.synchronize()
+    assert torch.equal(back.dr[-tail:], want.dr) and torch.equal(back.dy[-tail:], want.dy)
+
+
+def test_clip_of_more_than_2_31_elements():
+    """Only the ends of a tensor and another tensor are not zero: 3-4-12 gives 13, and every coefficient is 1 / 2."""
+    n = 2 ** 31 + 8195
+    g, other = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.full((1,), 12.0, device="cuda")
+    g[0], g[-1] = 3.0, 4.0
+    norm = M.mote_clip_grad_norm(M.GradClip([g, other]), 6.5)
+    torch.cuda.synchronize()
+    assert norm.item() == 13.0 and g[0].item() == 1.5 and g[-1].item() == 2.0 and other.item() == 6.0
+    assert int((g != 0).sum()) == 2
