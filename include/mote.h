@@ -201,8 +201,9 @@ mote_status mote_router_balance(const void* x, const void* w_router, const float
  * expert_counts out: int32 [E] or NULL; number of (token, slot) pairs of each expert
  * score_sum    out: fp32 [E] or NULL; sum over the tokens of s (fp64 sums in a fixed order): with expert_counts the two
  *                   factors of Eq.12
- * workspace       : device, >= mote_route_workspace_bytes(T, d, E), 256-byte aligned; up to 64 tokens it may be NULL when
- *                   expert_counts and score_sum are
+ * workspace       : device, >= mote_route_workspace_bytes(T, d, E), 256-byte aligned; up to 64 tokens it may be NULL (or
+ *                   smaller) when expert_counts and score_sum are; wide rows are slower then, and weights may differ in
+ *                   the last bits
  * Limits: d % 128 == 0, d <= 65536, 1 <= E <= 64, T * top_k < 2^24; T == 0 leaves counts and sums zero.
  * Softmax without groups, bias and renormalise selects as mote_router_topk does (finite logits). */
 enum { MOTE_SCORE_SOFTMAX = 0, MOTE_SCORE_SIGMOID = 1 };

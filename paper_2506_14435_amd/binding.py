@@ -557,7 +557,7 @@ def mote_route(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRouting, se
     if want_stats:
         counts = torch.empty(n_exp, dtype=torch.int32, device=dev)
         score_sum = torch.empty(n_exp, dtype=torch.float32, device=dev)
-    if want_stats or n_tok > 64:
+    if want_stats or n_tok > 64 or d * (32 + n_exp) >= 1 << 17:   # needed, or faster: channels to several workgroups
         workspace = _workspace(workspace, load_library().mote_route_workspace_bytes(n_tok, d, n_exp), dev)
     _call("mote_route", n, ctypes.byref(routing.struct), _addr(x), _addr(w_router), _addr(select_bias), _addr(token_mask), n_tok, d,
           n_exp, _addr(idx), _addr(wt), _addr(logits), _addr(counts), _addr(score_sum), _addr(workspace),

@@ -224,7 +224,8 @@ struct RouteArgs {
 };
 constexpr int kRouteFewTokens = 64;
 size_t route_workspace_bytes(int T, int d, int E, bool stats);
-hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, hipStream_t stream);
+size_t route_split_bytes(int T, int d, int E);   // what a split over the channels takes behind that, 0: none
+hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, bool split, hipStream_t stream);
 struct RouteBackwardArgs {
   const uint16_t* x;
   const uint16_t* w_router;

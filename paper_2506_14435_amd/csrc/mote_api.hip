@@ -786,7 +786,7 @@ mote_status mote_ste_linear_backward(const void* dy, const int32_t* offsets_host
 
 size_t mote_route_workspace_bytes(int T, int d, int E) {
   if (T < 0 || T >= (1 << 24) || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
-  return route_workspace_bytes(T, d, E, true);
+  return route_workspace_bytes(T, d, E, true) + route_split_bytes(T, d, E);
 }
 
 mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_router, const float* select_bias,
@@ -808,7 +808,10 @@ mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_rou
   RouteArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_router), select_bias, token_mask, T, d, E, k,
               cfg->score == MOTE_SCORE_SIGMOID, G, cfg->top_groups, cfg->group_top, cfg->renormalise != 0, cfg->scale,
               topk_idx, topk_w, logits, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
-  MOTE_HIP(launch_route(a, expert_counts, score_sum, workspace, static_cast<hipStream_t>(hip_stream)));
+  const size_t split = route_split_bytes(T, d, E);
+  const bool may_split = split > 0 && workspace && reinterpret_cast<uintptr_t>(workspace) % kAlign == 0 &&
+                         workspace_bytes >= (stats ? route_workspace_bytes(T, d, E, true) : 0) + split;
+  MOTE_HIP(launch_route(a, expert_counts, score_sum, workspace, may_split, static_cast<hipStream_t>(hip_stream)));
   return MOTE_OK;
 }
 

@@ -437,17 +437,16 @@ __device__ __forceinline__ float dot2(uint32_t v, float c) {
 // unit come as they lie in memory, NL loads of 16 bytes a lane (8 NL >= E), and are turned into the operands of NF = 2 through
 // LDS.  PAIRS: E is even, two experts of a row are one aligned word.  (Loading those words from memory takes the
 // address unit as long for four bytes as for 16: 580 cycles a unit, of 36 loads instead of 12.)
+// The logits' sums of units [u_lo, u_hi), one set per wavefront, in lds.red (a barrier is still to come), the norms' shares in
+// lds.nx, nw, orx and orw.
 template <int NF, bool LAID, int NL, bool PAIRS>
-__global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
-  __shared__ __attribute__((aligned(16))) RouteLds lds;
+__device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, int u_lo, int u_hi) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r = lane & 31, g = lane >> 5;
   const int t0 = blockIdx.x * kRtTokens;
   // neighbouring units go to one wavefront: at any time the eight read places of a row that lie far apart (rows are often a
   // multiple of 4096 bytes, and so are the places of one memory channel)
-  const int units = a.d / kRtUnit, u_begin = wave * units / kRtWaves, u_end = (wave + 1) * units / kRtWaves;
-  if (tid < 64) lds.cnt[tid] = 0;
-  if (tid < kRtTokens * 9) (&lds.sel[0][0])[tid] = -1;
+  const int units = a.d / kRtUnit, u_begin = u_lo + wave * (u_hi - u_lo) / kRtWaves, u_end = u_lo + (wave + 1) * (u_hi - u_lo) / kRtWaves;
 
   // 16-byte pieces of the tokens' units: eight lanes read the 128 bytes of a token, piece p of token t goes to place p ^ (t & 7) of
   // its 128 bytes of LDS, which spreads the operand reads (32 tokens, one piece) over the banks.  (Operands straight from memory
@@ -578,42 +577,64 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
   for (int f = 0; f < NF; ++f)
 #pragma unroll
     for (int v = 0; v < 16; ++v) lds.red[wave][64 * (16 * f + v) + lane] = acc[f][v];
-  if (wave == 0) {
-    // |w|^2 of expert `lane`; a bound that is not a number must not get lost in the maximum
-    float n = 0.0f;
-    uint32_t any = 0;
-#pragma unroll
-    for (int i = 0; i < kRtWaves; ++i) {
-      n += LAID ? lds.nw[i][lane] : lds.nw[i][lane] + lds.nw[i][lane + 64];
-      any |= lds.orw[i];
-    }
-    n = lane < a.E ? (n == n ? n : INFINITY) : 0.0f;
-    n = row_max(n);
-    n = fmaxf(n, __shfl_xor(n, 16, 64));
-    n = fmaxf(n, __shfl_xor(n, 32, 64));
-    if (lane == 0) lds.w2 = any ? fmaxf(n, 0x1p-149f) : 0.0f;
-  } else if (wave == 1 && lane < kRtTokens) {
-    float n = 0.0f;
-    uint32_t any = 0;
-#pragma unroll
-    for (int i = 0; i < kRtWaves; ++i) {
-      n += lds.nx[i][lane];
-      any |= lds.orx[i][lane];
-    }
-    lds.x2[lane] = any ? fmaxf(n == n ? n : INFINITY, 0x1p-149f) : 0.0f;   // zero only for zeros
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 2 * NF; ++i) {
-    const int at = tid + i * kRtThreads;
-    double sum = lds.red[0][at];
-#pragma unroll
-    for (int w = 1; w < kRtWaves; ++w) sum += lds.red[w][at];
-    const int v = at >> 6, ln = at & 63;
-    lds.l[(v & 3) + 8 * ((v >> 2) & 3) + 4 * (ln >> 5)][NF == 2 ? 2 * (ln & 31) + (v >> 4) : ln & 31] = sum;
-  }
-  __syncthreads();
+}
 
+// Sums over the wavefronts in their order: |w|^2 of expert `lane` and |x|^2 of token `lane`, and element `at` of lds.red, which is
+// the logit of token_of(at) and expert_of(at).
+template <bool LAID>
+__device__ __forceinline__ float expert_norm(const RouteLds& lds, uint32_t& any) {
+  const int lane = threadIdx.x & 63;
+  float n = 0.0f;
+  any = 0;
+#pragma unroll
+  for (int i = 0; i < kRtWaves; ++i) {
+    n += LAID ? lds.nw[i][lane] : lds.nw[i][lane] + lds.nw[i][lane + 64];
+    any |= lds.orw[i];
+  }
+  return n;
+}
+__device__ __forceinline__ float token_norm(const RouteLds& lds, uint32_t& any) {
+  const int lane = threadIdx.x & 31;
+  float n = 0.0f;
+  any = 0;
+#pragma unroll
+  for (int i = 0; i < kRtWaves; ++i) {
+    n += lds.nx[i][lane];
+    any |= lds.orx[i][lane];
+  }
+  return n;
+}
+__device__ __forceinline__ double element_sum(const RouteLds& lds, int at) {
+  double sum = lds.red[0][at];
+#pragma unroll
+  for (int w = 1; w < kRtWaves; ++w) sum += lds.red[w][at];
+  return sum;
+}
+__device__ __forceinline__ int token_of(int at) { return ((at >> 6) & 3) + 8 * ((at >> 8) & 3) + 4 * ((at >> 5) & 1); }
+template <int NF> __device__ __forceinline__ int expert_of(int at) { return NF == 2 ? 2 * (at & 31) + (at >> 10) : at & 31; }
+
+// The largest |w|^2 and the tokens' |x|^2 for the bound: one that is not a number must not get lost in the maximum, and zero
+// stands for zeros only.
+__device__ __forceinline__ void put_w2(const RouteArgs& a, RouteLds& lds, float n, uint32_t any) {
+  const int lane = threadIdx.x & 63;
+  n = lane < a.E ? (n == n ? n : INFINITY) : 0.0f;
+  n = row_max(n);
+  n = fmaxf(n, __shfl_xor(n, 16, 64));
+  n = fmaxf(n, __shfl_xor(n, 32, 64));
+  if (lane == 0) lds.w2 = any ? fmaxf(n, 0x1p-149f) : 0.0f;
+}
+__device__ __forceinline__ void put_x2(RouteLds& lds, float n, uint32_t any) {
+  lds.x2[threadIdx.x & 31] = any ? fmaxf(n == n ? n : INFINITY, 0x1p-149f) : 0.0f;
+}
+__device__ __forceinline__ void route_start(RouteLds& lds) {
+  if (threadIdx.x < 64) lds.cnt[threadIdx.x] = 0;
+  if (threadIdx.x < kRtTokens * 9) (&lds.sel[0][0])[threadIdx.x] = -1;
+}
+
+// From the logits (lds.l) to the outputs
+template <bool LAID>
+__device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * kRtTokens, units = a.d / kRtUnit;
   // Selection: 16 lanes per token, all 32 at once.
   const int t = tid >> 4, s = tid & 15, tok = t0 + t;
   const bool live = tok < a.T;
@@ -720,6 +741,87 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
   }
 }
 
+template <int NF, bool LAID, int NL, bool PAIRS>
+__global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
+  __shared__ __attribute__((aligned(16))) RouteLds lds;
+  const int tid = threadIdx.x, wave = tid >> 6;
+  route_start(lds);
+  route_logits<NF, LAID, NL, PAIRS>(a, lds, 0, a.d / kRtUnit);
+  uint32_t any;
+  if (wave == 0) {
+    const float n = expert_norm<LAID>(lds, any);
+    put_w2(a, lds, n, any);
+  } else if (wave == 1 && (tid & 63) < kRtTokens) {
+    const float n = token_norm(lds, any);
+    put_x2(lds, n, any);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2 * NF; ++i) {
+    const int at = tid + i * kRtThreads;
+    lds.l[token_of(at)][expert_of<NF>(at)] = element_sum(lds, at);
+  }
+  __syncthreads();
+  route_finish<LAID>(a, lds);
+}
+
+// A few tokens and many channels: the bytes of the router's rows and of the tokens, at the 30 a cycle that a CU takes in, are
+// what a workgroup's time is made of.  Shares of the channels (blockIdx.y) go to workgroups of their own, which leave their sums
+// and norms in memory, and a second kernel adds them in order and goes on.
+struct RoutePart {
+  double l[kRtTokens * 64];        // in the order of lds.red
+  float nx[kRtTokens], nw[64];
+  uint32_t orx[kRtTokens], orw, unused[31];
+};
+template <int NL, bool PAIRS>
+__global__ __launch_bounds__(kRtThreads) void route_part_kernel(RouteArgs a, RoutePart* __restrict__ parts) {
+  __shared__ __attribute__((aligned(16))) RouteLds lds;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, units = a.d / kRtUnit, share = blockIdx.y, shares = gridDim.y;
+  RoutePart& out = parts[blockIdx.x * shares + share];
+  route_logits<2, false, NL, PAIRS>(a, lds, share * units / shares, (share + 1) * units / shares);
+  uint32_t any;
+  if (wave == 0) {
+    out.nw[lane] = expert_norm<false>(lds, any);
+    if (lane == 0) out.orw = any;
+  } else if (wave == 1 && lane < kRtTokens) {
+    out.nx[lane] = token_norm(lds, any);
+    out.orx[lane] = any;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out.l[tid + i * kRtThreads] = element_sum(lds, tid + i * kRtThreads);
+}
+__global__ __launch_bounds__(kRtThreads) void route_join_kernel(RouteArgs a, const RoutePart* __restrict__ parts, int shares) {
+  __shared__ __attribute__((aligned(16))) RouteLds lds;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const RoutePart* const in = parts + static_cast<int64_t>(blockIdx.x) * shares;
+  route_start(lds);
+  double sum[4] = {};
+  float n = 0.0f;
+  uint32_t any = 0;
+#pragma unroll 4
+  for (int s = 0; s < shares; ++s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += in[s].l[tid + i * kRtThreads];
+    if (wave == 0) {
+      n += in[s].nw[lane];
+      any |= in[s].orw;
+    } else if (wave == 1 && lane < kRtTokens) {
+      n += in[s].nx[lane];
+      any |= in[s].orx[lane];
+    }
+  }
+  if (wave == 0) put_w2(a, lds, n, any);
+  else if (wave == 1 && lane < kRtTokens) put_x2(lds, n, any);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int at = tid + i * kRtThreads;
+    lds.l[token_of(at)][expert_of<2>(at)] = sum[i];
+  }
+  __syncthreads();
+  route_finish<false>(a, lds);
+}
+
 // Counts and score sums of all workgroups in a fixed order: 16 experts per workgroup, 64 slices of the partial sums.
 __global__ __launch_bounds__(1024) void route_stats_kernel(const double* __restrict__ part_sum, const int32_t* __restrict__ part_cnt, int blocks,
                                                            int E, int32_t* __restrict__ counts, float* __restrict__ score_sum) {
@@ -754,6 +856,18 @@ static int route_blocks(int T) { return (T + kRtTokens - 1) / kRtTokens; }
 static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
 static int route_operands(int E) { return E <= 32 ? 1 : 2; }
 
+// Shares of the channels for up to kRouteFewTokens tokens: a unit for each wavefront, 16 at most (d = 16384, E = 64: 16 shares 18.7 us,
+// 32 of them 24.4), from 256 KB of operands for a workgroup of 32 tokens on (below, the second launch takes what it saves).  One
+// workgroup, and split, in us: d = 1280, E = 64 12.3, 12.8; 2048 x 64 14.1, 12.3; 3584 x 64 19.1, 14.0; 7168 x 64 30.0, 16.9;
+// 2048 x 32 13.5, 11.7; 4096 x 16 16.3, 12.5; 1024 x 8 8.6, 9.9.
+static int route_shares(int T, int d, int E) {
+  return T > 0 && T <= kRouteFewTokens && d * (kRtTokens + E) >= 1 << 17 ? std::min(d / (kRtUnit * kRtWaves), 16) : 1;
+}
+size_t route_split_bytes(int T, int d, int E) {
+  const int shares = route_shares(T, d, E);
+  return shares > 1 ? align256(static_cast<size_t>(route_blocks(T)) * shares * sizeof(RoutePart)) : 0;
+}
+
 size_t route_workspace_bytes(int T, int d, int E, bool stats) {
   size_t n = 0;
   if (stats) n += align256(static_cast<size_t>(route_blocks(T)) * 64 * (sizeof(double) + sizeof(int32_t)) + 1);
@@ -761,7 +875,7 @@ size_t route_workspace_bytes(int T, int d, int E, bool stats) {
   return n;
 }
 
-hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, hipStream_t stream) {
+hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, bool split, hipStream_t stream) {
   const int blocks = route_blocks(a.T), units = a.d / kRtUnit;
   const bool stats = counts != nullptr || score_sum != nullptr;
   char* ws = static_cast<char*>(workspace);
@@ -787,6 +901,15 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
       route_layout_kernel<2><<<units, kLayThreads, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
       route_kernel<2, true, 8, true><<<blocks, kRtThreads, 0, stream>>>(a);
     }
+  } else if (split) {
+    const int shares = route_shares(a.T, a.d, a.E);
+    RoutePart* const parts = reinterpret_cast<RoutePart*>(ws);
+    const dim3 grid(blocks, shares);
+    if (a.E <= 16 && a.E % 2 == 0) route_part_kernel<2, true><<<grid, kRtThreads, 0, stream>>>(a, parts);
+    else if (a.E <= 16) route_part_kernel<2, false><<<grid, kRtThreads, 0, stream>>>(a, parts);
+    else if (a.E % 2 == 0) route_part_kernel<8, true><<<grid, kRtThreads, 0, stream>>>(a, parts);
+    else route_part_kernel<8, false><<<grid, kRtThreads, 0, stream>>>(a, parts);
+    route_join_kernel<<<blocks, kRtThreads, 0, stream>>>(a, parts, shares);
   } else if (a.T > 0) {
     if (a.E <= 16 && a.E % 2 == 0) route_kernel<2, false, 2, true><<<blocks, kRtThreads, 0, stream>>>(a);
     else if (a.E <= 16) route_kernel<2, false, 2, false><<<blocks, kRtThreads, 0, stream>>>(a);

@@ -111,6 +111,32 @@ def test_route_groups(E, G, top, gt, k, score):
         _check_route(x, w, b, None, k, score=score, n_groups=G, top_groups=top, group_top=gt, renormalise=True)
 
 
+# few tokens, rows so wide that the channels go to several workgroups; d / 64 that the shares do not divide, odd E, more shares than waves
+@pytest.mark.parametrize("T,d,E,k", [(1, 4096, 16, 2), (64, 2048, 33, 8), (17, 3456, 7, 3), (40, 8320, 64, 8), (33, 16384, 5, 2), (2, 65536, 64, 6)])
+def test_route_of_wide_rows(T, d, E, k):
+    g, x, w = _router(T, d, E, T + d + E)
+    bias = torch.randn(E, generator=g) * 0.05
+    mask = (torch.rand(T, generator=g) < 0.7).to(torch.uint8)
+    _check_route(x, w, None, None, k)
+    _check_route(x, w, bias, mask, k, score="sigmoid", renormalise=True)
+    # pairs of columns that fp32 sums cannot tell apart, and one that is the same
+    w[:, 1] = w[:, 0]
+    w[:, 3] = w[:, 2]
+    x[:, d - 1] = (torch.randn(T, generator=g) * 2.0 ** -20).to(torch.bfloat16)
+    w[d - 1, 1] = 1.0
+    cfg = dict(score="softmax", renormalise=True)
+    _check_route(x, w, None, None, k, **cfg)
+    # the call without memory for shares: the same experts
+    args = (x.cuda(), w.cuda(), M.MoteRouting(k, **cfg))
+    one, many = M.mote_route(*args, workspace=torch.empty(256, dtype=torch.uint8, device="cuda")), M.mote_route(*args)
+    torch.cuda.synchronize()
+    assert torch.equal(one.topk_idx, many.topk_idx) and torch.allclose(one.topk_w, many.topk_w, rtol=U * 200, atol=0)
+    x[0, d // 2] = math.nan
+    r = M.mote_route(x.cuda(), w.cuda(), M.MoteRouting(k), want_stats=True)
+    torch.cuda.synchronize()
+    assert ((r.topk_idx >= 0) & (r.topk_idx < E)).all() and r.topk_w[0].isnan().all() and not r.topk_w[1:].isnan().any()
+
+
 def test_route_agrees_with_the_plain_router():
     for T, d, E, k in ((64, 256, 4, 2), (300, 896, 8, 2), (2000, 2048, 16, 2), (100, 384, 40, 8)):
         _, x, w = _router(T, d, E, T)
