@@ -217,12 +217,12 @@ struct RouteArgs {
   float* logits;            // or null
   double* part_sum;         // per workgroup: score sums [64] and counts [64], or null
   int32_t* part_cnt;
-  const unsigned int __attribute__((ext_vector_type(4)))* ops;   // the router's weights as MFMA operands, more than kRouteFewTokens tokens
+  const unsigned int __attribute__((ext_vector_type(4)))* ops;   // the router's weights as MFMA operands (route_layout_kernel), or null
   const unsigned int __attribute__((ext_vector_type(4)))* cols;  // and as columns [E, d]
   const float* op_w2;       // per unit of channels and expert: sum of squares, and the bits of the values
   const uint32_t* op_bits;
 };
-constexpr int kRouteFewTokens = 64;
+constexpr int kRouteFewTokens = 64;   // what needs no workspace
 size_t route_workspace_bytes(int T, int d, int E, bool stats);
 size_t route_split_bytes(int T, int d, int E);   // what a split over the channels takes behind that, 0: none
 hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, bool split, hipStream_t stream);

@@ -433,7 +433,7 @@ __device__ __forceinline__ float dot2(uint32_t v, float c) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, v), __builtin_bit_cast(bf16x2, v), c, false);
 }
 
-// LAID: the router's weights come as operands, from route_layout_kernel.  Otherwise (a few tokens: one launch) the rows of a
+// LAID: the router's weights come as operands, from route_layout_kernel.  Otherwise (up to kRouteUnlaidTokens: one launch) the rows of a
 // unit come as they lie in memory, NL loads of 16 bytes a lane (8 NL >= E), and are turned into the operands of NF = 2 through
 // LDS.  PAIRS: E is even, two experts of a row are one aligned word.  (Loading those words from memory takes the
 // address unit as long for four bytes as for 16: 580 cycles a unit, of 36 loads instead of 12.)
@@ -765,7 +765,7 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
   route_finish<LAID>(a, lds);
 }
 
-// A few tokens and many channels: the bytes of the router's rows and of the tokens, at the 30 a cycle that a CU takes in, are
+// Few tokens and many channels: the bytes of the router's rows and of the tokens, at the 30 a cycle that a CU takes in, are
 // what a workgroup's time is made of.  Shares of the channels (blockIdx.y) go to workgroups of their own, which leave their sums
 // and norms in memory, and a second kernel adds them in order and goes on.
 struct RoutePart {
@@ -856,12 +856,17 @@ static int route_blocks(int T) { return (T + kRtTokens - 1) / kRtTokens; }
 static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
 static int route_operands(int E) { return E <= 32 ? 1 : 2; }
 
-// Shares of the channels for up to kRouteFewTokens tokens: a unit for each wavefront, 16 at most (d = 16384, E = 64: 16 shares 18.7 us,
-// 32 of them 24.4), from 256 KB of operands for a workgroup of 32 tokens on (below, the second launch takes what it saves).  One
+// Up to this many tokens the workgroups are too few for the chip, and weights that are laid out first come too late: their kernel
+// takes longer than it saves.  One kernel, or split, and laid out first, in us, 128 tokens: 896 x 8 8.9, 9.8; 2048 x 16 11.4, 11.8;
+// 2048 x 64 12.4, 15.0; 3584 x 64 13.8, 19.5; 1024 tokens: 9.1, 10.0; 11.6, 12.1; 17.3, 19.3; 28.1, 29.9; 2048 x 3584 x 64 27.7, 25.2.
+constexpr int kRouteUnlaidTokens = 1024;
+// Shares of the channels: a unit for each wavefront, 16 at most (d = 16384, E = 64: 16 shares 18.7 us, 32 of them 24.4), a workgroup
+// per CU at most, from 256 KB of operands for a workgroup of 32 tokens on (below, the second launch takes what it saves).  One
 // workgroup, and split, in us: d = 1280, E = 64 12.3, 12.8; 2048 x 64 14.1, 12.3; 3584 x 64 19.1, 14.0; 7168 x 64 30.0, 16.9;
 // 2048 x 32 13.5, 11.7; 4096 x 16 16.3, 12.5; 1024 x 8 8.6, 9.9.
 static int route_shares(int T, int d, int E) {
-  return T > 0 && T <= kRouteFewTokens && d * (kRtTokens + E) >= 1 << 17 ? std::min(d / (kRtUnit * kRtWaves), 16) : 1;
+  if (T == 0 || T > kRouteUnlaidTokens || d * (kRtTokens + E) < 1 << 17) return 1;
+  return std::min({d / (kRtUnit * kRtWaves), 16, 256 / route_blocks(T)});
 }
 size_t route_split_bytes(int T, int d, int E) {
   const int shares = route_shares(T, d, E);
@@ -884,7 +889,9 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
     a.part_cnt = reinterpret_cast<int32_t*>(a.part_sum + static_cast<int64_t>(blocks) * 64);
     ws += align256(static_cast<size_t>(blocks) * 64 * (sizeof(double) + sizeof(int32_t)) + 1);
   }
-  if (a.T > kRouteFewTokens) {
+  // odd E: two experts of a row are two words (3584 x 63 37 us, laid out 19)
+  const bool lay = a.T > kRouteUnlaidTokens || (a.T > kRouteFewTokens && !split && (route_shares(a.T, a.d, a.E) > 1 || (a.E > 16 && a.E % 2 != 0)));
+  if (lay) {
     const int nf = route_operands(a.E);
     u4* const ops = reinterpret_cast<u4*>(ws);
     u4* const cols = ops + static_cast<int64_t>(units) * 4 * nf * 64;

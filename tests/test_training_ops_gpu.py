@@ -137,6 +137,45 @@ def test_route_of_wide_rows(T, d, E, k):
     assert ((r.topk_idx >= 0) & (r.topk_idx < E)).all() and r.topk_w[0].isnan().all() and not r.topk_w[1:].isnan().any()
 
 
+@pytest.mark.parametrize("T,d,E,k", [(70, 7168, 64, 8), (200, 2048, 64, 6), (1024, 3584, 9, 2), (333, 2176, 35, 4)])
+@pytest.mark.parametrize("split", [True, False])
+def test_route_of_wide_rows_and_some_tokens(T, d, E, k, split):
+    """Memory for shares of the channels or not: an equal pair of columns, a pair that fp32 sums cannot tell apart, a padded batch."""
+    g, x, w = _router(T, d, E, T + d + E)
+    w[:, 1] = w[:, 0]
+    w[:, 3] = w[:, 2]
+    x[:, d - 1] = (torch.randn(T, generator=g) * 2.0 ** -20).to(torch.bfloat16)
+    w[d - 1, 1] = 1.0
+    mask = (torch.rand(T, generator=g) < 0.7).to(torch.uint8)
+    ref = O.route(_np(x), _np(w), k, token_mask=mask.numpy(), renormalise=True)
+    need = M.load_library().mote_route_workspace_bytes(T, d, E)
+    r = M.mote_route(x.cuda(), w.cuda(), M.MoteRouting(k, renormalise=True), token_mask=mask.cuda(), want_stats=True,
+                     workspace=torch.empty(need if split else need - 256, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    same = _same_selection(r.topk_idx.cpu().numpy(), ref, x, w, None)
+    # logits are off by e and rounded scores by 64 roundings: weights by exp(2 e)
+    e = 2.0 ** -20 * (np.abs(_np(x)) @ np.abs(_np(w))).max(axis=1)
+    _close(r.topk_w[torch.from_numpy(same)], ref["w"][same], (2 * e + 128 * U)[same, None] * ref["w"][same] + TINY, "weights")
+    assert int(r.counts.sum()) == k * int(mask.sum())
+
+
+# the kernel of many tokens, whose weights are laid out first
+@pytest.mark.parametrize("E", [32, 64])
+@pytest.mark.parametrize("gap", [2.0 ** -8, 2.0 ** -34])
+def test_route_tells_close_logits_of_many_tokens_apart(gap, E):
+    test_route_tells_close_logits_apart(gap, 1050, E)
+
+
+@pytest.mark.parametrize("E", [6, 40])
+def test_route_separates_three_and_more_of_many_tokens(E):
+    test_route_separates_three_and_more(1040, E)
+
+
+@pytest.mark.parametrize("E", [12, 44, 45])
+def test_route_large_small_and_nonfinite_values_of_many_tokens(E):
+    test_route_large_small_and_nonfinite_values(1033, E)
+
+
 def test_route_agrees_with_the_plain_router():
     for T, d, E, k in ((64, 256, 4, 2), (300, 896, 8, 2), (2000, 2048, 16, 2), (100, 384, 40, 8)):
         _, x, w = _router(T, d, E, T)
