@@ -450,7 +450,8 @@ __device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, 
 
   // 16-byte pieces of the tokens' units: eight lanes read the 128 bytes of a token, piece p of token t goes to place p ^ (t & 7) of
   // its 128 bytes of LDS, which spreads the operand reads (32 tokens, one piece) over the banks.  (Operands straight from memory
-  // touch the 32 rows four times each: 8192 x 2048 50000 cycles instead of 23000 up to the logits.)
+  // touch the 32 rows four times each: 8192 x 2048 50000 cycles instead of 23000 up to the logits.)  The whole offset is the lane's: a
+  // scalar offset has no part in the range check, and tokens behind the last one must not be read.
   const uint32_t x_bytes = 2u * a.d;
   const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.x) + static_cast<int64_t>(t0) * a.d, 0,
                                                                       static_cast<int>(min(a.T - t0, kRtTokens) * x_bytes), 0x00020000);   // zeros behind the last token
@@ -463,9 +464,9 @@ __device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, 
     u = min(u, u_end - 1);
     const uint32_t base = static_cast<uint32_t>(u) * (LAID ? 4u * NF * 1024u : kRtUnit * row_bytes);
 #pragma unroll
-    for (int i = 0; i < NL; ++i) q.w[i] = __builtin_amdgcn_raw_buffer_load_b128(rw, 16 * lane + 1024 * i, base, 0);   // zeros behind the last row
+    for (int i = 0; i < NL; ++i) q.w[i] = __builtin_amdgcn_raw_buffer_load_b128(rw, 16 * lane + base + 1024 * i, 0, 0);   // zeros behind the last row
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q.x[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, x_lane, static_cast<uint32_t>(8 * i) * x_bytes + 2u * kRtUnit * u, 0);
+    for (int i = 0; i < 4; ++i) q.x[i] = __builtin_amdgcn_raw_buffer_load_b128(rx, x_lane + (static_cast<uint32_t>(8 * i) * x_bytes + 2u * kRtUnit * u), 0, 0);
     __builtin_amdgcn_sched_barrier(0);   // the loads of a unit leave before the work on the one in front of it
     return q;
   };
