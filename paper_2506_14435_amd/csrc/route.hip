@@ -232,13 +232,18 @@ __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_
 // The same for one token by a whole wavefront (lane e: expert e), on fp64 keys: the rare case, compact rather than fast.
 // exact: bit e, the logit of expert e is settled; the others are off by tol.  Returns the experts whose logits have to be
 // settled for the selection to be that of fp64 logits (0: it is final, sel is written).
+// The keys of settled experts are as good as fp64, but for softmax scores with something added: the denominator has the logits of
+// all experts in it.  An error of tol in those that are not settled moves it by a factor 1 + r, |r| <= (exp(tol) - 1) times the sum of
+// their scores, and with it the difference of two keys by r times that of their scores.  Where that could change their order, the
+// experts with the larger ones of those scores are settled too, round by round, until it cannot.
 __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const double* l_row, double* key_row, double* grp_row, int* sel, float tol,
                                                        uint64_t exact) {
   const int e = threadIdx.x & 63, E = a.E;
   const double kNone = -INFINITY, slack = 0x1p-50;
   const float width = 2.0f * key_tolerance(a, tol);
+  const bool shared = !a.sigmoid && !keys_are_logits(a);
   const double l = e < E ? l_row[e] : kNone;
-  double key = l;
+  double key = l, score = 0.0;
   if (!keys_are_logits(a)) {
     if (a.sigmoid) {
       key = 1.0 / (1.0 + exp(-l));
@@ -246,25 +251,36 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
       key = exp(l - wave_max(l));
       if (e >= E) key = 0.0;
       key /= wave_add(key);
+      score = key;
     }
     if (a.bias && e < E) key += static_cast<double>(a.bias[e]);
   }
   if (key != key) key = -DBL_MAX;
   if (e >= E) key = kNone;
-  uint64_t more = 0;
+  uint64_t more = 0, heavy = 0;   // heavy: of the scores that are not settled those around their mean and above, one at least
+  double moved = 0.0;             // bounds |r|
+  if (shared) {
+    const bool open = e < E && !((exact >> e) & 1);
+    const double mass = wave_add(open ? score : 0.0), mean = mass / static_cast<double>(max(E - __builtin_popcountll(exact), 1));
+    moved = mass * (tol < 0.05f ? 1.1f * tol : INFINITY);
+    heavy = __ballot(open && !(score < 0.99 * mean));
+  }
   if (a.n_groups > 1) {
     const int G = a.n_groups, n = E / G;
     key_row[e] = key;
+    grp_row[e] = score;
     wave_lds_fence();
-    double t1 = kNone, t2 = kNone;
+    double t1 = kNone, t2 = kNone, mass = 0.0;   // mass: all scores of the group, at least those in its key
     if (e < G)
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
         const double kv = key_row[e * n + j];
         t2 = fmax(t2, fmin(kv, t1));
         t1 = fmax(t1, kv);
+        mass += grp_row[e * n + j];
       }
     const double gs = a.group_top == 2 ? t1 + t2 : t1;
+    wave_lds_fence();
     grp_row[e] = gs;
     wave_lds_fence();
     key_row[e] = a.group_top == 2 ? t2 : t1;   // the smallest key of the group's score
@@ -280,9 +296,14 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
     const double mine = grp_row[min(e / n, G - 1)];
     const float w = width * static_cast<float>(a.group_top);
     const double least = key_row[min(e / n, G - 1)];
-    if (best_out > kNone && near_keys(worst_in, best_out, w, slack))   // what makes the scores of the groups around the border
+    if (best_out > kNone && near_keys(worst_in, best_out, w, slack)) {   // what makes the scores of the groups around the border
       more |= __ballot(key > kNone && (key > least || near_keys(key, least, width, slack)) &&
                        (near_keys(mine, worst_in, w, slack) || near_keys(mine, best_out, w, slack)));
+      if (shared && (more & ~exact) == 0) {
+        const double most = wave_max(e < G && (near_keys(gs, worst_in, w, slack) || near_keys(gs, best_out, w, slack)) ? mass : 0.0);
+        if (!(worst_in - best_out > most * moved)) more |= heavy;
+      }
+    }
     if (e < E && !((open >> (e / n)) & 1)) key = kNone;
   }
   const double first = key;
@@ -295,8 +316,12 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
     if (e == j) got = win;
     if (e == win) key = kNone;
     // experts whose key may lie on the other side of this one, itself included
-    const uint64_t at = __ballot(first > kNone && near_keys(first, m, width, slack));
-    if (__builtin_popcountll(at) > 1) more |= at;
+    const bool close = first > kNone && near_keys(first, m, width, slack);
+    const uint64_t at = __ballot(close);
+    if (__builtin_popcountll(at) > 1) {
+      more |= at;
+      if (shared && (at & ~exact) == 0 && __ballot(close && !(fabs(first - m) >= fabs(score - __shfl(score, win, kWave)) * moved))) more |= heavy;
+    }
   }
   if (e < 8) sel[e] = got;
   return more & ~exact;

@@ -33,3 +33,45 @@ def test_route_of_operands_among_other_data(T, d, E):
             assert torch.equal(a, b)
     ref = O.route(_np(x), _np(w), k, renormalise=True)
     assert np.array_equal(outs[0].topk_idx.cpu().numpy(), ref["idx"])
+
+
+def _two_of_different_scores(T, d, E, seed, groups):
+    """Tokens that are one token but for a channel that only the other experts see: experts a and b have quite different scores and
+    a bias that brings their keys (with groups: the scores of their groups) together, so that the rows' denominators order them."""
+    g, x, w = _router(1, d, E, seed)
+    x[0, torch.randperm(d - 1, generator=g)[:4]] *= 20.0
+    w = (w.float() * 0.3).to(torch.bfloat16)
+    x = x.expand(T, d).clone()
+    x[:, d - 1] = (torch.randn(T, generator=g) * 2.0 ** -22).to(torch.bfloat16)
+    x[0, d - 1] = 0.0
+    w[d - 1] = torch.randn(E, generator=g).to(torch.bfloat16)
+    logits = _np(x[:1]) @ _np(w)
+    s = np.exp(logits[0] - logits[0].max())
+    s /= s.sum()
+    bias = torch.zeros(E)
+    if groups == 1:
+        a, b = np.argsort(-s)[[0, 12]]
+        w[d - 1, [a, b]] = 0.0
+        bias[b] = float(s[a] - s[b])
+    else:
+        n = E // groups
+        top2 = np.sort(s.reshape(groups, n), axis=1)[:, -2:].sum(axis=1)
+        ga, gb = np.argsort(-top2)[[0, groups // 2]]
+        w[d - 1, n * ga:n * ga + n] = 0.0
+        w[d - 1, n * gb:n * gb + n] = 0.0
+        best = n * gb + np.argmax(s[n * gb:n * gb + n])
+        bias[best] = float(top2[ga] - top2[gb])                        # the two groups' scores meet
+    return x, w, bias
+
+
+@pytest.mark.parametrize("T", [32, 1056])                              # the kernel of few tokens and that of many
+@pytest.mark.parametrize("groups,k", [(1, 1), (1, 4), (8, 4)])
+def test_route_orders_keys_that_hang_on_the_denominator(T, groups, k):
+    """Softmax scores with a bias: the key of an expert whose own logit is settled still moves with the other experts' logits."""
+    cfg = dict(n_groups=groups, top_groups=1, group_top=2) if groups > 1 else {}
+    flips = 0
+    for seed in range(6):
+        x, w, bias = _two_of_different_scores(T, 2048, 64, seed, groups)
+        ref, _ = _check_route(x, w, bias, None, k, **cfg)
+        flips += len(np.unique(ref["idx"][:, 0])) > 1
+    assert flips >= 3                                                  # tokens of one batch fall on either side
