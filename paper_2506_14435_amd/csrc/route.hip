@@ -78,10 +78,10 @@ __device__ __forceinline__ float value_of(int o) { return __int_as_float(o ^ ((o
 __device__ __forceinline__ bool keys_are_logits(const RouteArgs& a) { return a.bias == nullptr && !(a.n_groups > 1 && a.group_top == 2); }
 
 // How far a key may be off where the logits are off by tol: the score's slope is at most a quarter (sigmoid) or twice the score
-// (softmax).  Not for large tol, where a slope says nothing.
-__device__ __forceinline__ float key_tolerance(const RouteArgs& a, float tol) {
+// (softmax), of which none is above `most`.  Not for large tol, where a slope says nothing.
+__device__ __forceinline__ float key_tolerance(const RouteArgs& a, float tol, float most) {
   if (keys_are_logits(a)) return tol;
-  return tol < 0.05f ? (a.sigmoid ? 0.25f : 2.2f) * tol : INFINITY;
+  return tol < 0.05f ? (a.sigmoid ? 0.25f : 2.2f * most) * tol : INFINITY;
 }
 template <typename R>
 __device__ __forceinline__ bool near_keys(R x, R y, float width, R slack) {
@@ -118,12 +118,13 @@ __device__ __forceinline__ void route_scores(const RouteArgs& a, const double* l
 // 1 .. k, only the experts sel[j - 1] and sel[j] are too close to be told apart; -1, more hangs on logits that are off by
 // `tol` and scores by the rounding of exp_of and rcp.
 // key_row, grp_row: 64 integers of LDS each (groups only).
-__device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_row, const float (&sc)[4], double shift, int* key_row, int* grp_row,
+__device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_row, const float (&sc)[4], double shift, float total, int* key_row, int* grp_row,
                                             int* sel, float tol) {
   const int s = threadIdx.x & 15, E = a.E;
   const bool by_logit = keys_are_logits(a);
-  float delta = key_tolerance(a, tol);
-  if (!by_logit) delta += (a.sigmoid ? 8.0f : 16.0f + 4.0f * fabsf(static_cast<float>(shift))) * 0x1p-24f;
+  const float most = a.sigmoid ? 1.0f : 1.001f / total;   // the largest score
+  float delta = key_tolerance(a, tol, most);
+  if (!by_logit) delta += (a.sigmoid ? 8.0f : most * (16.0f + 4.0f * fabsf(static_cast<float>(shift)))) * 0x1p-24f;
   const float slack = 4 * 0x1p-24f;
   int key[4];
 #pragma unroll
@@ -240,7 +241,6 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
                                                        uint64_t exact) {
   const int e = threadIdx.x & 63, E = a.E;
   const double kNone = -INFINITY, slack = 0x1p-50;
-  const float width = 2.0f * key_tolerance(a, tol);
   const bool shared = !a.sigmoid && !keys_are_logits(a);
   const double l = e < E ? l_row[e] : kNone;
   double key = l, score = 0.0;
@@ -257,6 +257,7 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
   }
   if (key != key) key = -DBL_MAX;
   if (e >= E) key = kNone;
+  const float width = 2.0f * key_tolerance(a, tol, shared ? static_cast<float>(wave_max(score)) * 1.001f : 1.0f);
   uint64_t more = 0, heavy = 0;   // heavy: of the scores that are not settled those around their mean and above, one at least
   double moved = 0.0;             // bounds |r|
   if (shared) {
@@ -675,7 +676,7 @@ __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) 
   float sc[4], total;
   double shift;
   route_scores(a, lds.l[t], sc, shift, total);
-  int state = route_select(a, lds.l[t], sc, shift, reinterpret_cast<int*>(lds.pick.key[t]), reinterpret_cast<int*>(lds.pick.grp[t]), lds.sel[t], tol);
+  int state = route_select(a, lds.l[t], sc, shift, total, reinterpret_cast<int*>(lds.pick.key[t]), reinterpret_cast<int*>(lds.pick.grp[t]), lds.sel[t], tol);
   if (vague || (state > 0 && (zero || !(a.sigmoid || keys_are_logits(a))))) state = -1;
   if (!live || masked) state = 0;
   // Rare: the logits that a selection hangs on are settled by the token's wavefront.  Two experts are put in order; otherwise the
