@@ -48,8 +48,6 @@ template <typename T, typename F> __device__ __forceinline__ T row_reduce(T v, F
   return f(v, dpp<0x140>(v));
 }
 __device__ __forceinline__ int row_max(int v) { return row_reduce(v, [](int a, int b) { return max(a, b); }); }
-__device__ __forceinline__ int row_min(int v) { return row_reduce(v, [](int a, int b) { return min(a, b); }); }
-__device__ __forceinline__ int row_or(int v) { return row_reduce(v, [](int a, int b) { return a | b; }); }
 __device__ __forceinline__ float row_max(float v) { return row_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ double row_max(double v) { return row_reduce(v, [](double a, double b) { return fmax(a, b); }); }
 template <typename T> __device__ __forceinline__ T row_sum(T v) { return row_reduce(v, [](T a, T b) { return a + b; }); }
@@ -117,7 +115,7 @@ __device__ __forceinline__ void route_scores(const RouteArgs& a, const double* l
 // has filled with -1, and the first one that is not to sel[k].  Returns in every lane of the row: 0, the selection is final; j in
 // 1 .. k, only the experts sel[j - 1] and sel[j] are too close to be told apart; -1, more hangs on logits that are off by
 // `tol` and scores by the rounding of exp_of and rcp.
-// key_row, grp_row: 64 integers of LDS each (groups only).
+// key_row, grp_row: 64 and 128 integers of LDS (groups only).
 __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_row, const float (&sc)[4], double shift, float total, int* key_row, int* grp_row,
                                             int* sel, float tol) {
   const int s = threadIdx.x & 15, E = a.E;
@@ -141,7 +139,7 @@ __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_
 #pragma unroll
     for (int v = 0; v < 4; ++v) key_row[s + 16 * v] = key[v];
     wave_lds_fence();
-    int worst_in = INT_MAX, best_out = kNoKey;
+    float worst_in = INFINITY, best_out = -INFINITY;   // the least that a group inside, the most that one outside may have
     uint64_t open = 0;
 #pragma unroll 1
     for (int i = 0; 16 * i < G; ++i) {
@@ -160,8 +158,15 @@ __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_
         }
       }
       int gs = t1;
-      if (a.group_top == 2) gs = t2 == kNoKey ? kNoKey : order_of(value_of(t1) + value_of(t2));
-      if (g < G) grp_row[g] = gs;
+      float lost = slack * fabsf(value_of(t1));   // by rounding the keys and their sum: of the size of the keys, which may cancel
+      if (a.group_top == 2) {
+        gs = t2 == kNoKey ? kNoKey : order_of(value_of(t1) + value_of(t2));
+        lost += slack * fabsf(value_of(t2));
+      }
+      if (g < G) {
+        grp_row[g] = gs;
+        grp_row[64 + g] = __float_as_int(lost);
+      }
     }
     wave_lds_fence();
 #pragma unroll 1
@@ -177,17 +182,18 @@ __device__ __forceinline__ int route_select(const RouteArgs& a, const double* l_
         for (int q = 0; q < 8; ++q) rank += j + q < G && (o[q] > gs || (o[q] == gs && j + q < g)) ? 1 : 0;
       }
       const bool in = g < G && rank < a.top_groups;
-      if (g < G) {
-        if (in) worst_in = min(worst_in, gs);
-        else best_out = max(best_out, gs);
+      if (g < G && gs != kNoKey) {
+        const float lost = __int_as_float(grp_row[64 + g]), score = value_of(gs);   // +inf inside: a NaN, which fminf passes over
+        if (in) worst_in = fminf(worst_in, score - lost);
+        else best_out = fmaxf(best_out, score + lost);
       }
       open |= ((__ballot(in) >> (threadIdx.x & 48)) & 0xFFFFull) << (16 * i);
     }
-    worst_in = row_min(worst_in);
+    worst_in = -row_max(-worst_in);
     best_out = row_max(best_out);
     const float width = 2.0f * static_cast<float>(a.group_top) * delta;
     const unsigned inv_n = 65536u / static_cast<unsigned>(n) + 1u;   // e / n for e < 64
-    many = best_out != kNoKey && near_keys(value_of(worst_in), value_of(best_out), width, slack);
+    many = !(worst_in - best_out > width);   // also where both are below the range of fp32
 #pragma unroll
     for (int v = 0; v < 4; ++v)
       if (!((open >> (((s + 16 * v) * inv_n) >> 16)) & 1)) key[v] = kNoKey;

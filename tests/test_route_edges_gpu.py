@@ -75,3 +75,20 @@ def test_route_orders_keys_that_hang_on_the_denominator(T, groups, k):
         ref, _ = _check_route(x, w, bias, None, k, **cfg)
         flips += len(np.unique(ref["idx"][:, 0])) > 1
     assert flips >= 3                                                  # tokens of one batch fall on either side
+
+
+@pytest.mark.parametrize("T", [64, 1056])
+@pytest.mark.parametrize("E,groups", [(8, 4), (48, 6)])
+@pytest.mark.parametrize("size", [1e2, 1e3, 1e4, 1e6])
+def test_route_groups_whose_keys_cancel(T, E, groups, size):
+    """A group's score of a large key and one as large below zero: what its fp32 sum has lost is of the keys' size, not of the sum's."""
+    g, x, w = _router(T, 256, E, int(size) + E)
+    n = E // groups
+    bias = torch.zeros(E)
+    bias[0::n] = size * (1 + torch.rand(groups, generator=g))
+    bias[1::n] = -bias[0::n]
+    for i in range(2, n):                                              # of more than two, the others are below
+        bias[i::n] = -4 * size
+    for score in ("softmax", "sigmoid"):
+        ref, _ = _check_route(x, w, bias, None, 4, score=score, n_groups=groups, top_groups=2, group_top=2)
+        assert len(np.unique(ref["idx"] // n)) == groups               # no group is always in
