@@ -219,7 +219,8 @@ struct RouteArgs {
   int32_t* part_cnt;
   const unsigned int __attribute__((ext_vector_type(4)))* ops;   // the router's weights as MFMA operands (route_layout_kernel), or null
   const unsigned int __attribute__((ext_vector_type(4)))* cols;  // and as columns [E, d]
-  const float* op_w2;       // per unit of channels and expert: sum of squares, and the bits of the values
+  const float* op_w2;       // per unit of channels and expert: sum of squares, sum of squared powers of two, bits of the values
+  const float* op_q2;
   const uint32_t* op_bits;
 };
 constexpr int kRouteFewTokens = 64;   // what needs no workspace

@@ -807,7 +807,7 @@ mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_rou
   if (T == 0 && !stats) return MOTE_OK;
   RouteArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_router), select_bias, token_mask, T, d, E, k,
               cfg->score == MOTE_SCORE_SIGMOID, G, cfg->top_groups, cfg->group_top, cfg->renormalise != 0, cfg->scale,
-              topk_idx, topk_w, logits, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
+              topk_idx, topk_w, logits, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
   const size_t split = route_split_bytes(T, d, E);
   const bool may_split = split > 0 && workspace && reinterpret_cast<uintptr_t>(workspace) % kAlign == 0 &&
                          workspace_bytes >= (stats ? route_workspace_bytes(T, d, E, true) : 0) + split;

@@ -21,12 +21,14 @@ constexpr int kRtWaves = 8;
 constexpr int kRtThreads = 64 * kRtWaves;
 constexpr int kRtUnit = 64;       // channels of a unit
 constexpr int kRtRow = 65;        // elements of an LDS row of 64 logits or keys: the rows of a wavefront's four tokens start in different banks
-// How far a logit may be off, in units of 2^-24 |x| |w| (Euclidean norms, which bound sum |x w|).  A unit is a chain of four
-// instructions, each of which aligns 16 products and the addend to the largest of them.  Measured against the unit's own
-// |x| |w|, over normal, one-signed, wide-range and one-large inputs: at most 6.0 units (1.3 for normal ones), of which at most
-// 1.6 have one sign in all units of a row; the rest adds up like random signs.  Taken: 3 for the first and 6 / sqrt(units) for
-// the second, plus one for the rounding of the logit to fp32.
-__device__ __forceinline__ float logit_bound(int units) { return (4.0f + 6.0f * __builtin_amdgcn_rsqf(static_cast<float>(units))) * 0x1p-24f * 1.02f; }
+// How far a logit may be off.  An instruction adds its 16 channels in two steps of eight; a step cuts the products (and a smaller
+// addend) at 2^-24 of the largest product's exponent, adds them and rounds to fp32 (read off the instruction with products that cancel).
+// In units of 2^-24, with Euclidean norms: step j = 0 .. 7 of a unit is off by at most 8 |x_j| q_j, q the largest power of two not above
+// any |w| of its eight channels, and by the sum so far, at most that of |x_i| |w_i| over the steps i <= j.  For all units that is
+//   8 |x| sqrt(sum q^2) + sqrt(sum ((8 - j) |x_j|)^2) |w|     (of normal values 3.9 + 5.1 |x| |w|)
+// however the values lie; without the q's, where they would have to be found in the loop, sqrt(sum ((16 - j) |x_j|)^2) |w|, 12.8.
+// (Measured: one unit of products that take each other's bits is off by 11.1 |x| |w|, 0.93 of the bound.)
+constexpr float kLogitBound = 0x1p-24f * 1.05f;
 
 // LDS written and read by lanes of one wavefront
 __device__ __forceinline__ void wave_lds_fence() {
@@ -347,9 +349,10 @@ struct RouteLds {
     } pick;
   };
   double l[kRtTokens][kRtRow];                 // finished logits
-  float nx[kRtWaves][kRtTokens], nw[kRtWaves][128]; // shares of |x|^2 of the tokens and of |w|^2 of the experts (two each)
+  float nx[kRtWaves][kRtTokens], px[kRtWaves][kRtTokens];   // shares of the tokens' sums
+  float nw[kRtWaves][128];                     // shares of |w|^2 of the experts (two each), or of |w|^2 and the sum of q^2
   uint32_t orx[kRtWaves][kRtTokens], orw[kRtWaves]; // bits of the values: all zero or not
-  float x2[kRtTokens], w2;                     // |x|^2, the largest |w|^2; 0: nothing but zeros
+  float x2[kRtTokens], p2[kRtTokens], w2, q2;  // sums of the tokens, the largest ones of the experts; x2, w2 0: nothing but zeros
   int sel[kRtTokens][9];
   int cnt[64];
 };
@@ -358,13 +361,13 @@ static_assert(sizeof(RouteLds) <= 160 * 1024, "LDS of a CU");
 // The router's weights as the operands of route_kernel: for a unit of 64 channels, operand f of step s is 64 lanes of 16
 // bytes, lane 32 g + r: channels 16 s + 8 g .. + 7 of expert r (NF = 1, E <= 32) or 2 r + f (NF = 2).  And as columns [E, d],
 // for logits that are settled (reading them out of the operands, a line of memory for 16 bytes, took 13000 cycles for two).
-// One unit per workgroup, which also leaves every expert's share of |w|^2 and the bits of its values.
+// One unit per workgroup, which also leaves every expert's shares of |w|^2 and of the sum of q^2 and the bits of its values.
 constexpr int kLayThreads = 1024;   // four elements and one or two pieces a thread: the kernel is a chain of latencies
 template <int NF>
 __global__ __launch_bounds__(kLayThreads) void route_layout_kernel(const uint16_t* __restrict__ w, int d, int E, u4* __restrict__ ops, u4* __restrict__ cols,
-                                                                   float* __restrict__ w2, uint32_t* __restrict__ bits) {
+                                                                   float* __restrict__ w2, float* __restrict__ q2, uint32_t* __restrict__ bits) {
   __shared__ uint16_t s_w[kRtUnit][64 + 2];
-  __shared__ float s_n[16][64];
+  __shared__ float s_n[16][64], s_q[16][64];
   __shared__ uint32_t s_any[16][64];
   const int u = blockIdx.x, tid = threadIdx.x, e = tid & 63, part = tid >> 6;
   const uint16_t* const src = w + static_cast<int64_t>(u) * kRtUnit * E;
@@ -372,14 +375,16 @@ __global__ __launch_bounds__(kLayThreads) void route_layout_kernel(const uint16_
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = e < E ? src[(4 * part + i) * E + e] : 0;
   float n = 0.0f;
-  uint32_t any = 0;
+  uint32_t any = 0, q = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     s_w[4 * part + i][e] = v[i];
     n = fmaf(bf16_to_f32(v[i]), bf16_to_f32(v[i]), n);
     any |= v[i] & 0x7FFFu;
+    q = max(q, v[i] & 0x7F80u);
   }
   s_n[part][e] = n;
+  s_q[part][e] = __uint_as_float(q << 16);
   s_any[part][e] = any;
   __syncthreads();
   // the lower threads write the operands, the upper ones the columns: eight channels of an expert each
@@ -396,12 +401,16 @@ __global__ __launch_bounds__(kLayThreads) void route_layout_kernel(const uint16_
   if (part == 0) {
     n = 0.0f;
     any = 0;
+    float sum_q = 0.0f;
 #pragma unroll
-    for (int q = 0; q < 16; ++q) {
-      n += s_n[q][e];
-      any |= s_any[q][e];
+    for (int j = 0; j < 16; j += 2) {   // eight channels
+      n += s_n[j][e] + s_n[j + 1][e];
+      any |= s_any[j][e] | s_any[j + 1][e];
+      const float most = fmaxf(s_q[j][e], s_q[j + 1][e]);
+      sum_q = fmaf(most, most, sum_q);
     }
     w2[u * 64 + e] = n;
+    q2[u * 64 + e] = sum_q;
     bits[u * 64 + e] = any;
   }
 }
@@ -509,7 +518,7 @@ __device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, 
   for (int f = 0; f < NF; ++f)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[f][v] = 0.0;
-  float nx[4] = {}, nw[NF] = {};   // nx, orx: tokens 8 i + lane / 8
+  float nx[4] = {}, nw[NF] = {};   // nx, orx: tokens 8 i + lane / 8, step lane % 8 of the units
   uint32_t orx[4] = {}, orw = 0;
   unsigned char* const x_stage = lds.stage.x[wave];
   const unsigned char* const x_row = x_stage + r * 128;
@@ -565,11 +574,12 @@ __device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, 
       for (int v = 0; v < 16; ++v) acc[f][v] += static_cast<double>(c[f][v]);
     wave_lds_fence();
   };
-  float op_n = 0.0f;   // LAID: this wavefront's share of the units' |w|^2 of expert `lane`
+  float op_n = 0.0f, op_q = 0.0f;   // LAID: this wavefront's shares of the units' |w|^2 and sum of q^2 of expert `lane`
   uint32_t op_any = 0;
   if constexpr (LAID)
     for (int u = wave; u < units; u += kRtWaves) {
       op_n += a.op_w2[u * 64 + lane];
+      op_q += a.op_q2[u * 64 + lane];
       op_any |= a.op_bits[u * 64 + lane];
     }
   if (u_begin < u_end) {
@@ -586,12 +596,17 @@ __device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, 
   // Sums over the wavefronts in their order.  Element v of a lane is token (v & 3) + 8 (v >> 2) + 4 g of the lane's expert.
 #pragma unroll
   for (int i = 0; i < 4; ++i) {   // over the eight lanes of a token
-    float n = nx[i];
+    const float share = static_cast<float>((LAID ? 8 : 16) - (lane & 7));
+    float n = nx[i] * (share * share), p = nx[i];
     int o = static_cast<int>(orx[i] & 0x7FFF7FFFu);
     n += dpp<0xB1>(n); n += dpp<0x4E>(n); n += dpp<0x141>(n);
+    if constexpr (LAID) {
+      p += dpp<0xB1>(p); p += dpp<0x4E>(p); p += dpp<0x141>(p);
+    }
     o |= dpp<0xB1>(o); o |= dpp<0x4E>(o); o |= dpp<0x141>(o);
     if ((lane & 7) == 0) {
       lds.nx[wave][8 * i + (lane >> 3)] = n;
+      if constexpr (LAID) lds.px[wave][8 * i + (lane >> 3)] = p;
       lds.orx[wave][8 * i + (lane >> 3)] = o;
     }
   }
@@ -602,6 +617,7 @@ __device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, 
     if (lane == 0) lds.orw[wave] = any_w;
   } else {
     lds.nw[wave][lane] = op_n;
+    lds.nw[wave][64 + lane] = op_q;
     op_any = __ballot(op_any != 0) != 0;
     if (lane == 0) lds.orw[wave] = op_any;
   }
@@ -612,30 +628,35 @@ __device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, 
     for (int v = 0; v < 16; ++v) lds.red[wave][64 * (16 * f + v) + lane] = acc[f][v];
 }
 
-// Sums over the wavefronts in their order: |w|^2 of expert `lane` and |x|^2 of token `lane`, and element `at` of lds.red, which is
-// the logit of token_of(at) and expert_of(at).
+// Sums over the wavefronts in their order: |w|^2 (and the sum of q^2) of expert `lane`, those of token
+// `lane`, and element `at` of lds.red, which is the logit of token_of(at) and expert_of(at).
+struct Norms {
+  float n, p;
+  uint32_t any;
+};
 template <bool LAID>
-__device__ __forceinline__ float expert_norm(const RouteLds& lds, uint32_t& any) {
+__device__ __forceinline__ Norms expert_norm(const RouteLds& lds) {
   const int lane = threadIdx.x & 63;
-  float n = 0.0f;
-  any = 0;
+  Norms r{};
 #pragma unroll
   for (int i = 0; i < kRtWaves; ++i) {
-    n += LAID ? lds.nw[i][lane] : lds.nw[i][lane] + lds.nw[i][lane + 64];
-    any |= lds.orw[i];
+    r.n += LAID ? lds.nw[i][lane] : lds.nw[i][lane] + lds.nw[i][lane + 64];
+    if constexpr (LAID) r.p += lds.nw[i][lane + 64];
+    r.any |= lds.orw[i];
   }
-  return n;
+  return r;
 }
-__device__ __forceinline__ float token_norm(const RouteLds& lds, uint32_t& any) {
+template <bool LAID>
+__device__ __forceinline__ Norms token_norm(const RouteLds& lds) {
   const int lane = threadIdx.x & 31;
-  float n = 0.0f;
-  any = 0;
+  Norms r{};
 #pragma unroll
   for (int i = 0; i < kRtWaves; ++i) {
-    n += lds.nx[i][lane];
-    any |= lds.orx[i][lane];
+    r.n += lds.nx[i][lane];
+    if constexpr (LAID) r.p += lds.px[i][lane];
+    r.any |= lds.orx[i][lane];
   }
-  return n;
+  return r;
 }
 __device__ __forceinline__ double element_sum(const RouteLds& lds, int at) {
   double sum = lds.red[0][at];
@@ -646,18 +667,26 @@ __device__ __forceinline__ double element_sum(const RouteLds& lds, int at) {
 __device__ __forceinline__ int token_of(int at) { return ((at >> 6) & 3) + 8 * ((at >> 8) & 3) + 4 * ((at >> 5) & 1); }
 template <int NF> __device__ __forceinline__ int expert_of(int at) { return NF == 2 ? 2 * (at & 31) + (at >> 10) : at & 31; }
 
-// The largest |w|^2 and the tokens' |x|^2 for the bound: one that is not a number must not get lost in the maximum, and zero
+// The experts' largest and the tokens' own sums for the bound: one that is not a number must not get lost in the maximum, and zero
 // stands for zeros only.
-__device__ __forceinline__ void put_w2(const RouteArgs& a, RouteLds& lds, float n, uint32_t any) {
-  const int lane = threadIdx.x & 63;
-  n = lane < a.E ? (n == n ? n : INFINITY) : 0.0f;
+__device__ __forceinline__ float expert_max(const RouteArgs& a, float n) {
+  n = static_cast<int>(threadIdx.x & 63) < a.E ? (n == n ? n : INFINITY) : 0.0f;
   n = row_max(n);
   n = fmaxf(n, __shfl_xor(n, 16, 64));
-  n = fmaxf(n, __shfl_xor(n, 32, 64));
-  if (lane == 0) lds.w2 = any ? fmaxf(n, 0x1p-149f) : 0.0f;
+  return fmaxf(n, __shfl_xor(n, 32, 64));
 }
-__device__ __forceinline__ void put_x2(RouteLds& lds, float n, uint32_t any) {
-  lds.x2[threadIdx.x & 31] = any ? fmaxf(n == n ? n : INFINITY, 0x1p-149f) : 0.0f;
+template <bool LAID>
+__device__ __forceinline__ void put_w2(const RouteArgs& a, RouteLds& lds, const Norms& r) {
+  const float n = expert_max(a, r.n);
+  if ((threadIdx.x & 63) == 0) lds.w2 = r.any ? fmaxf(n, 0x1p-149f) : 0.0f;
+  if constexpr (LAID) {
+    const float q = expert_max(a, r.p);
+    if ((threadIdx.x & 63) == 0) lds.q2 = q;
+  }
+}
+__device__ __forceinline__ void put_x2(RouteLds& lds, const Norms& r) {
+  lds.x2[threadIdx.x & 31] = r.any ? fmaxf(r.n == r.n ? r.n : INFINITY, 0x1p-149f) : 0.0f;
+  lds.p2[threadIdx.x & 31] = r.p;
 }
 __device__ __forceinline__ void route_start(RouteLds& lds) {
   if (threadIdx.x < 64) lds.cnt[threadIdx.x] = 0;
@@ -667,7 +696,7 @@ __device__ __forceinline__ void route_start(RouteLds& lds) {
 // From the logits (lds.l) to the outputs
 template <bool LAID>
 __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * kRtTokens, units = a.d / kRtUnit;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * kRtTokens;
   // Selection: 16 lanes per token, all 32 at once.
   const int t = tid >> 4, s = tid & 15, tok = t0 + t;
   const bool live = tok < a.T;
@@ -675,7 +704,9 @@ __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) 
   // squares that underflow say nothing; products below the smallest normal value are off by an absolute amount
   const float x2 = lds.x2[t], w2 = lds.w2;
   bool zero = x2 == 0.0f || w2 == 0.0f;   // all logits are exactly zero
-  float tol = logit_bound(units) * sqrtf(x2) * sqrtf(w2) + 0x1p-120f;
+  float tol = sqrtf(x2) * sqrtf(w2);
+  if constexpr (LAID) tol += 8.0f * sqrtf(lds.p2[t]) * sqrtf(lds.q2);
+  tol = kLogitBound * tol + 0x1p-120f;
   if (!(x2 > 0x1p-80f && w2 > 0x1p-80f)) tol = INFINITY;
   if (zero) tol = 0.0f;
   const bool vague = !(tol < INFINITY);   // the bound says nothing: every logit of the token is settled
@@ -780,14 +811,8 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
   const int tid = threadIdx.x, wave = tid >> 6;
   route_start(lds);
   route_logits<NF, LAID, NL, PAIRS>(a, lds, 0, a.d / kRtUnit);
-  uint32_t any;
-  if (wave == 0) {
-    const float n = expert_norm<LAID>(lds, any);
-    put_w2(a, lds, n, any);
-  } else if (wave == 1 && (tid & 63) < kRtTokens) {
-    const float n = token_norm(lds, any);
-    put_x2(lds, n, any);
-  }
+  if (wave == 0) put_w2<LAID>(a, lds, expert_norm<LAID>(lds));
+  else if (wave == 1 && (tid & 63) < kRtTokens) put_x2(lds, token_norm<LAID>(lds));
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 2 * NF; ++i) {
@@ -812,13 +837,14 @@ __global__ __launch_bounds__(kRtThreads) void route_part_kernel(RouteArgs a, Rou
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, units = a.d / kRtUnit, share = blockIdx.y, shares = gridDim.y;
   RoutePart& out = parts[blockIdx.x * shares + share];
   route_logits<2, false, NL, PAIRS>(a, lds, share * units / shares, (share + 1) * units / shares);
-  uint32_t any;
   if (wave == 0) {
-    out.nw[lane] = expert_norm<false>(lds, any);
-    if (lane == 0) out.orw = any;
+    const Norms r = expert_norm<false>(lds);
+    out.nw[lane] = r.n;
+    if (lane == 0) out.orw = r.any;
   } else if (wave == 1 && lane < kRtTokens) {
-    out.nx[lane] = token_norm(lds, any);
-    out.orx[lane] = any;
+    const Norms r = token_norm<false>(lds);
+    out.nx[lane] = r.n;
+    out.orx[lane] = r.any;
   }
   __syncthreads();
 #pragma unroll
@@ -830,22 +856,21 @@ __global__ __launch_bounds__(kRtThreads) void route_join_kernel(RouteArgs a, con
   const RoutePart* const in = parts + static_cast<int64_t>(blockIdx.x) * shares;
   route_start(lds);
   double sum[4] = {};
-  float n = 0.0f;
-  uint32_t any = 0;
+  Norms r{};
 #pragma unroll 4
   for (int s = 0; s < shares; ++s) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum[i] += in[s].l[tid + i * kRtThreads];
     if (wave == 0) {
-      n += in[s].nw[lane];
-      any |= in[s].orw;
+      r.n += in[s].nw[lane];
+      r.any |= in[s].orw;
     } else if (wave == 1 && lane < kRtTokens) {
-      n += in[s].nx[lane];
-      any |= in[s].orx[lane];
+      r.n += in[s].nx[lane];
+      r.any |= in[s].orx[lane];
     }
   }
-  if (wave == 0) put_w2(a, lds, n, any);
-  else if (wave == 1 && lane < kRtTokens) put_x2(lds, n, any);
+  if (wave == 0) put_w2<false>(a, lds, r);
+  else if (wave == 1 && lane < kRtTokens) put_x2(lds, r);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int at = tid + i * kRtThreads;
@@ -909,7 +934,7 @@ size_t route_split_bytes(int T, int d, int E) {
 size_t route_workspace_bytes(int T, int d, int E, bool stats) {
   size_t n = 0;
   if (stats) n += align256(static_cast<size_t>(route_blocks(T)) * 64 * (sizeof(double) + sizeof(int32_t)) + 1);
-  if (T > kRouteFewTokens) n += align256(static_cast<size_t>(d / kRtUnit) * (4 * route_operands(E) * 1024 + 64 * 8) + static_cast<size_t>(E) * d * 2);
+  if (T > kRouteFewTokens) n += align256(static_cast<size_t>(d / kRtUnit) * (4 * route_operands(E) * 1024 + 64 * 12) + static_cast<size_t>(E) * d * 2);
   return n;
 }
 
@@ -929,16 +954,18 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
     u4* const ops = reinterpret_cast<u4*>(ws);
     u4* const cols = ops + static_cast<int64_t>(units) * 4 * nf * 64;
     float* const w2 = reinterpret_cast<float*>(cols + static_cast<int64_t>(a.E) * a.d / 8);
-    uint32_t* const bits = reinterpret_cast<uint32_t*>(w2 + units * 64);
+    float* const q2 = w2 + units * 64;
+    uint32_t* const bits = reinterpret_cast<uint32_t*>(q2 + units * 64);
     a.ops = ops;
     a.cols = cols;
     a.op_w2 = w2;
+    a.op_q2 = q2;
     a.op_bits = bits;
     if (nf == 1) {
-      route_layout_kernel<1><<<units, kLayThreads, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
+      route_layout_kernel<1><<<units, kLayThreads, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, q2, bits);
       route_kernel<1, true, 4, true><<<blocks, kRtThreads, 0, stream>>>(a);
     } else {
-      route_layout_kernel<2><<<units, kLayThreads, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, bits);
+      route_layout_kernel<2><<<units, kLayThreads, 0, stream>>>(a.w_router, a.d, a.E, ops, cols, w2, q2, bits);
       route_kernel<2, true, 8, true><<<blocks, kRtThreads, 0, stream>>>(a);
     }
   } else if (split) {

@@ -92,3 +92,50 @@ def test_route_groups_whose_keys_cancel(T, E, groups, size):
     for score in ("softmax", "sigmoid"):
         ref, _ = _check_route(x, w, bias, None, 4, score=score, n_groups=groups, top_groups=2, group_top=2)
         assert len(np.unique(ref["idx"] // n)) == groups               # no group is always in
+
+
+@pytest.mark.parametrize("T,E", [(32, 16), (40, 64), (1056, 16), (1056, 64)])
+@pytest.mark.parametrize("at", [0, 64 * 17, 64 * 31])
+def test_route_settles_what_one_unit_of_channels_has_lost(T, E, at):
+    """x and w_router confined to 64 of 2048 channels, where one large product takes the last bits of what is added after it and a
+    second one cancels it: expert 3 loses 17 units of 2^-24 of a product, expert 5 gains 15."""
+    x, w = torch.zeros(T, 2048), torch.zeros(2048, E)
+    x[:, at:at + 64] = 2.0 ** -12
+    x[:, [at, at + 32]] = 1.0
+    x *= 2.0 ** (torch.arange(T) % 7 - 3)[:, None]
+    most = 255 / 256 * 2.0 ** -12
+    w[at, 3], w[at + 32, 3], w[at, 5], w[at + 32, 5] = 1.0, -1.0, 1.0, -1.0
+    for c in (*range(1, 8), *range(33, 40)):
+        w[at + c, 3], w[at + c, 5] = most, -most
+    w[at + 8:at + 32, 3] = most / 8
+    w[at + 8:at + 32, 5] = -most / 17
+    w[at + 40, 5] = 31.875 * 2.0 ** -12
+    for e in range(E):
+        if e not in (3, 5):
+            w[at + 41, e] = -0.25 - e / 64
+    x, w = x.to(torch.bfloat16), w.to(torch.bfloat16)
+    l = _np(x) @ _np(w)
+    gap = (l[:, 3] - l[:, 5]) / (_np(x)[:, at] * 2.0 ** -24)
+    assert ((0 < gap) & (gap < 2)).all()
+    for k in (1, 2):
+        ref, _ = _check_route(x, w, None, None, k)
+        assert (ref["idx"][:, 0] == 3).all()
+
+
+@pytest.mark.parametrize("T,E", [(64, 16), (64, 64), (1056, 64)])
+@pytest.mark.parametrize("spread", [0, 12])
+def test_route_tells_close_logits_of_one_unit_apart(T, E, spread):
+    """Pairs of columns that differ in one channel, all weight in 64 of 2048 channels, values over a wide range of exponents."""
+    g, x, w = _router(T, 2048, E, 7 + spread)
+    x[:, :640], x[:, 704:] = 0.0, 0.0
+    w[:640], w[704:] = 0.0, 0.0
+    w = (w.float() * 6).to(torch.bfloat16)
+    if spread:
+        x = (x.float() * 2.0 ** torch.randint(-spread, 1, x.shape, generator=g)).to(torch.bfloat16)
+    w[:, 1::2] = w[:, 0::2]
+    x[:, 650] = (torch.randn(T, generator=g) * 2.0 ** -20).to(torch.bfloat16)
+    w[650, 1::2] = torch.randn(E // 2, generator=g).to(torch.bfloat16)
+    bias = (torch.randn(E // 2, generator=g) * 0.05).repeat_interleave(2)
+    for b in (None, bias):
+        for cfg in (dict(), dict(score="sigmoid", renormalise=True), dict(n_groups=8, top_groups=4, group_top=2)):
+            _check_route(x, w, b, None, 8, **cfg)
