@@ -325,11 +325,12 @@ __device__ __forceinline__ uint64_t route_select_exact(const RouteArgs& a, const
     if (e == j) got = win;
     if (e == win) key = kNone;
     // experts whose key may lie on the other side of this one, itself included
-    const bool close = first > kNone && near_keys(first, m, width, slack);
+    const double won = __shfl(score, win, kWave);
+    const bool close = first > kNone && near_keys(first, m, shared ? key_tolerance(a, tol, static_cast<float>(score + won)) * 1.001f : width, slack);
     const uint64_t at = __ballot(close);
     if (__builtin_popcountll(at) > 1) {
       more |= at;
-      if (shared && (at & ~exact) == 0 && __ballot(close && !(fabs(first - m) >= fabs(score - __shfl(score, win, kWave)) * moved))) more |= heavy;
+      if (shared && (at & ~exact) == 0 && __ballot(close && !(fabs(first - m) >= fabs(score - won) * moved))) more |= heavy;
     }
   }
   if (e < 8) sel[e] = got;
@@ -415,51 +416,68 @@ __global__ __launch_bounds__(kLayThreads) void route_layout_kernel(const uint16_
   }
 }
 
-// fp64 logits of two experts of a token by one wavefront, half of it for each.  Code that a workgroup in fifty reaches is fetched
-// from memory when it does (some 1000 cycles for 64 bytes of it, under the stream of the hidden states): here and below it
-// is short rather than unrolled.
+// fp64 logits of two experts of a token by one wavefront, eight channels of both a lane and round (half a wavefront for each expert,
+// twice the rounds: 16301 x 3584 x 60 72.5 us instead of 69.7).  Code that a workgroup in fifty reaches is fetched from memory when
+// it does (some 1000 cycles for 64 bytes of it, under the stream of the hidden states): here and below it is short rather than unrolled.
 template <bool LAID>
 __device__ __forceinline__ void settle_two(const RouteArgs& a, int tok, int e0, int e1, double* l_row) {
-  const int lane = threadIdx.x & 63, e = lane < 32 ? e0 : e1;
+  const int lane = threadIdx.x & 63;
   const uint16_t* const xr = a.x + static_cast<int64_t>(tok) * a.d;
-  double s = 0.0;
+  double s0 = 0.0, s1 = 0.0;
 #pragma unroll 2
-  for (int c = 8 * (lane & 31); c < a.d; c += 8 * 32) {
+  for (int c = 8 * lane; c < a.d; c += 8 * 64) {
     const u4 x = *reinterpret_cast<const u4*>(xr + c);
-    u4 w;
+    u4 w[2];
     if constexpr (LAID) {
-      w = a.cols[(static_cast<int64_t>(e) * a.d + c) >> 3];
+      w[0] = a.cols[(static_cast<int64_t>(e0) * a.d + c) >> 3];
+      w[1] = a.cols[(static_cast<int64_t>(e1) * a.d + c) >> 3];
     } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        w[q] = a.w_router[static_cast<size_t>(c + 2 * q) * a.E + e] | static_cast<uint32_t>(a.w_router[static_cast<size_t>(c + 2 * q + 1) * a.E + e]) << 16;
+      for (int h = 0; h < 2; ++h) {
+        const uint16_t* const p = a.w_router + static_cast<size_t>(c) * a.E + (h ? e1 : e0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[h][q] = p[2 * q * a.E] | static_cast<uint32_t>(p[(2 * q + 1) * a.E]) << 16;
+      }
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {   // fp64 products: of large values, beyond fp32, they are finite
-      s = fma(static_cast<double>(bf16_lo(x[q])), static_cast<double>(bf16_lo(w[q])), s);
-      s = fma(static_cast<double>(bf16_hi(x[q])), static_cast<double>(bf16_hi(w[q])), s);
+      const double lo = bf16_lo(x[q]), hi = bf16_hi(x[q]);
+      s0 = fma(lo, static_cast<double>(bf16_lo(w[0][q])), s0);
+      s0 = fma(hi, static_cast<double>(bf16_hi(w[0][q])), s0);
+      s1 = fma(lo, static_cast<double>(bf16_lo(w[1][q])), s1);
+      s1 = fma(hi, static_cast<double>(bf16_hi(w[1][q])), s1);
     }
   }
-  s = row_sum(s);
-  s += __shfl_xor(s, 16, kWave);
-  if ((lane & 31) == 0) l_row[e] = s;
+  s0 = wave_add(s0);
+  s1 = wave_add(s1);
+  if (lane == 0) {
+    l_row[e0] = s0;
+    l_row[e1] = s1;
+  }
   wave_lds_fence();
 }
 
 // Puts the experts sel[j - 1] and sel[j], whose logits are settled, into their order; lanes 0 and 1 of the wavefront have one each.
-// Keys are logits or sigmoid scores: softmax scores of a row have a denominator, which takes route_select_exact.
-__device__ __forceinline__ void order_two(const RouteArgs& a, const double* l_row, int* sel, int j, int e0, int e1) {
-  const int e = (threadIdx.x & 63) == 0 ? e0 : e1;
-  double key = l_row[e];
+// A softmax score is exp(l - shift) / total with an fp32 total, off by `part` of it at most (the other logits' tol, 16 roundings of
+// the exponentials weighted by their shares, 6 of their sum): that moves the difference of two keys by `part` of the scores' difference.
+// False where this could change the order.
+__device__ __forceinline__ bool order_two(const RouteArgs& a, const double* l_row, int* sel, int j, int e0, int e1, double shift, float total, float tol) {
+  const int lane = threadIdx.x & 63, e = lane == 0 ? e0 : e1;
+  double key = l_row[e], score = 0.0;
   if (!keys_are_logits(a)) {
-    key = 1.0 / (1.0 + exp(-key));
+    score = exp(a.sigmoid ? -key : key - shift);
+    score = a.sigmoid ? 1.0 / (1.0 + score) : score / static_cast<double>(total);
+    key = score;
     if (a.bias) key += static_cast<double>(a.bias[e]);
   }
-  const double other = __shfl(key, 1, kWave);
-  if ((threadIdx.x & 63) == 0 && !(key > other || (key == other && e0 < e1))) {
+  const double other = __shfl(key, 1, kWave), apart = fabs(score - __shfl(score, 1, kWave));
+  const float part = a.sigmoid || keys_are_logits(a) ? 0.0f : (tol < 0.05f ? 1.1f * tol + 32 * 0x1p-24f : INFINITY);
+  if (__builtin_amdgcn_readfirstlane(static_cast<int>(fabs(key - other) < apart * part))) return false;
+  if (lane == 0 && !(key > other || (key == other && e0 < e1))) {
     sel[j - 1] = e1;
     sel[j] = e0;
   }
+  return true;
 }
 
 // 64 channels of the 32 tokens and the router's rows of these channels: operands (LAID) or the rows as they lie in memory
@@ -714,7 +732,7 @@ __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) 
   double shift;
   route_scores(a, lds.l[t], sc, shift, total);
   int state = route_select(a, lds.l[t], sc, shift, total, reinterpret_cast<int*>(lds.pick.key[t]), reinterpret_cast<int*>(lds.pick.grp[t]), lds.sel[t], tol);
-  if (vague || (state > 0 && (zero || !(a.sigmoid || keys_are_logits(a))))) state = -1;
+  if (vague || (state > 0 && zero)) state = -1;
   if (!live || masked) state = 0;
   // Rare: the logits that a selection hangs on are settled by the token's wavefront.  Two experts are put in order; otherwise the
   // selection is made again in fp64 until it hangs on no logit that is not settled.
@@ -737,8 +755,7 @@ __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) 
       if (st > 0) {
         const int e0 = __builtin_amdgcn_readfirstlane(sel[st - 1]), e1 = __builtin_amdgcn_readfirstlane(sel[st]);
         settle_two<LAID>(a, t0 + tq, e0, e1, l_row);
-        order_two(a, l_row, sel, st, e0, e1);
-        continue;
+        if (order_two(a, l_row, sel, st, e0, e1, __shfl(shift, 16 * q, kWave), __shfl(total, 16 * q, kWave), tol_q)) continue;
       }
       uint64_t exact = z ? all : 0, next = tol_q < INFINITY ? 0 : all;
       for (;;) {
