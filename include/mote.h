@@ -188,7 +188,8 @@ mote_status mote_router_balance(const void* x, const void* w_router, const float
  * switches it off) is never selected: slots that find no expert get index -1 and weight 0.  A NaN key ranks as the lowest
  * finite value: indices stay in range and the weights carry the NaN.  Indices follow from fp64 logits whatever kernel
  * computes them: sums whose rounding could matter are settled in fp64 before an index is written (keys of different columns
- * that fp64 itself rounds together may fall either way; equal columns go to the lower index).
+ * that fp64 itself rounds together may fall either way; equal columns go to the lower index).  The weights, the logits and
+ * the score sums that are returned come from fp32 sums over 64 channels, added in fp64.
  *
  * cfg          in : the description above; top_k <= 8 and at most the experts of top_groups groups, n_groups divides E,
  *                   group_top 1 or 2 and at most E / n_groups.  n_groups == 1: no groups (top_groups, group_top 1)
@@ -201,9 +202,11 @@ mote_status mote_router_balance(const void* x, const void* w_router, const float
  * expert_counts out: int32 [E] or NULL; number of (token, slot) pairs of each expert
  * score_sum    out: fp32 [E] or NULL; sum over the tokens of s (fp64 sums in a fixed order): with expert_counts the two
  *                   factors of Eq.12
- * workspace       : device, >= mote_route_workspace_bytes(T, d, E), 256-byte aligned; up to 64 tokens it may be NULL (or
- *                   smaller) when expert_counts and score_sum are; wide rows are slower then, and weights may differ in
- *                   the last bits
+ * workspace       : device, 256-byte aligned.  mote_route_workspace_bytes(T, d, E) bytes serve every batch of up to T tokens,
+ *                   mote_route_lean_workspace_bytes those calls whose expert_counts and score_sum are NULL (0: they use none).
+ *                   Up to 64 tokens a lean call may have none or less, and up to 1024 tokens a smaller workspace is taken if
+ *                   it holds the statistics and the weights laid out (MOTE_ERR_WORKSPACE_TOO_SMALL otherwise): wide rows are
+ *                   slower then, and logits and weights may differ in the last bits
  * Limits: d % 128 == 0, d <= 65536, 1 <= E <= 64, T * top_k < 2^24; T == 0 leaves counts and sums zero.
  * Softmax without groups, bias and renormalise selects as mote_router_topk does (finite logits). */
 enum { MOTE_SCORE_SOFTMAX = 0, MOTE_SCORE_SIGMOID = 1 };
@@ -217,6 +220,7 @@ typedef struct {
   float scale;      /* finite                                            */
 } mote_routing;
 size_t mote_route_workspace_bytes(int T, int d, int E);
+size_t mote_route_lean_workspace_bytes(int T, int d, int E);
 mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_router, const float* select_bias,
                        const uint8_t* token_mask, int T, int d, int E, int32_t* topk_idx, float* topk_w, float* logits,
                        int32_t* expert_counts, float* score_sum, void* workspace, size_t workspace_bytes,

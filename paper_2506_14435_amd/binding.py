@@ -24,7 +24,7 @@ EXPORTS = ("mote_status_string", "mote_version", "mote_packed_bytes", "mote_pack
            "mote_router_topk", "mote_layer_workspace_bytes", "mote_layer_forward", "mote_layer_forward_static",
            "mote_block_forward", "mote_router_balance", "mote_pack_binary", "mote_rtn_packed_bytes", "mote_pack_rtn",
            "mote_ste_backward_workspace_bytes", "mote_ste_linear_backward",
-           "mote_route_workspace_bytes", "mote_route", "mote_route_backward_workspace_bytes", "mote_route_backward",
+           "mote_route_workspace_bytes", "mote_route_lean_workspace_bytes", "mote_route", "mote_route_backward_workspace_bytes", "mote_route_backward",
            "mote_layer_forward_routed", "mote_residual_norm", "mote_residual_norm_workspace_bytes",
            "mote_residual_norm_backward", "mote_clip_grad_norm_workspace_bytes", "mote_clip_grad_norm",
            "mote_stage_timing", "mote_stage_times", "mote_event_pair_overhead", "mote_tuning_set", "mote_calib_copy")
@@ -130,6 +130,8 @@ def load_library() -> ctypes.CDLL:
                                              c_size_t, c_void_p]
     lib.mote_route_workspace_bytes.restype = c_size_t
     lib.mote_route_workspace_bytes.argtypes = [c_int, c_int, c_int]
+    lib.mote_route_lean_workspace_bytes.restype = c_size_t
+    lib.mote_route_lean_workspace_bytes.argtypes = [c_int, c_int, c_int]
     lib.mote_route.restype = c_int
     lib.mote_route.argtypes = [POINTER(MoteRoutingStruct), c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int,
                                c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
@@ -557,8 +559,10 @@ def mote_route(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRouting, se
     if want_stats:
         counts = torch.empty(n_exp, dtype=torch.int32, device=dev)
         score_sum = torch.empty(n_exp, dtype=torch.float32, device=dev)
-    if want_stats or n_tok > 64 or d * (32 + n_exp) >= 1 << 17:   # needed, or faster: channels to several workgroups
-        workspace = _workspace(workspace, load_library().mote_route_workspace_bytes(n_tok, d, n_exp), dev)
+    lib = load_library()
+    need = (lib.mote_route_workspace_bytes if want_stats else lib.mote_route_lean_workspace_bytes)(n_tok, d, n_exp)
+    if need > 0:
+        workspace = _workspace(workspace, need, dev)
     _call("mote_route", n, ctypes.byref(routing.struct), _addr(x), _addr(w_router), _addr(select_bias), _addr(token_mask), n_tok, d,
           n_exp, _addr(idx), _addr(wt), _addr(logits), _addr(counts), _addr(score_sum), _addr(workspace),
           workspace.numel() if workspace is not None else 0)

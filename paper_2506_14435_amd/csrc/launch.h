@@ -224,8 +224,12 @@ struct RouteArgs {
   const uint32_t* op_bits;
 };
 constexpr int kRouteFewTokens = 64;   // what needs no workspace
-size_t route_workspace_bytes(int T, int d, int E, bool stats);
-size_t route_split_bytes(int T, int d, int E);   // what a split over the channels takes behind that, 0: none
+// Workspace: the statistics' partial sums, and behind them either the shares of a split over the channels (0: there is none) or the
+// weights laid out (0: the call takes them as they lie).
+size_t route_stats_bytes(int T);
+size_t route_split_bytes(int T, int d, int E);
+size_t route_layout_bytes(int T, int d, int E);
+size_t route_workspace_bytes(int T, int d, int E, bool stats);   // what serves every number of tokens up to T
 hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, bool split, hipStream_t stream);
 struct RouteBackwardArgs {
   const uint16_t* x;

@@ -786,7 +786,12 @@ mote_status mote_ste_linear_backward(const void* dy, const int32_t* offsets_host
 
 size_t mote_route_workspace_bytes(int T, int d, int E) {
   if (T < 0 || T >= (1 << 24) || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
-  return route_workspace_bytes(T, d, E, true) + route_split_bytes(T, d, E);
+  return route_workspace_bytes(T, d, E, true);
+}
+
+size_t mote_route_lean_workspace_bytes(int T, int d, int E) {
+  if (T < 0 || T >= (1 << 24) || d <= 0 || d % 128 || d > 65536 || E < 1 || E > 64) return 0;
+  return route_workspace_bytes(T, d, E, false);
 }
 
 mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_router, const float* select_bias,
@@ -799,18 +804,17 @@ mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_rou
   if (G < 1 || G > E || E % G || cfg->top_groups < 1 || cfg->top_groups > G || cfg->group_top < 1 || cfg->group_top > 2) return MOTE_ERR_INVALID_ARG;
   if (G > 1 && (cfg->group_top > E / G || k > cfg->top_groups * (E / G))) return MOTE_ERR_UNSUPPORTED_SHAPE;
   if (T > 0 && (!x || !w_router || !topk_idx || !topk_w)) return MOTE_ERR_INVALID_ARG;
-  const bool stats = expert_counts || score_sum;
+  const bool stats = expert_counts || score_sum, aligned = workspace && reinterpret_cast<uintptr_t>(workspace) % kAlign == 0;
+  const size_t split = route_split_bytes(T, d, E), before = stats ? route_stats_bytes(T) : 0;
+  const bool may_split = split > 0 && aligned && workspace_bytes >= before + split;
   if (stats || T > kRouteFewTokens) {
-    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return MOTE_ERR_INVALID_ARG;
-    if (workspace_bytes < route_workspace_bytes(T, d, E, stats)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
+    if (!aligned) return MOTE_ERR_INVALID_ARG;
+    if (!may_split && workspace_bytes < before + route_layout_bytes(T, d, E)) return MOTE_ERR_WORKSPACE_TOO_SMALL;
   }
   if (T == 0 && !stats) return MOTE_OK;
   RouteArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(w_router), select_bias, token_mask, T, d, E, k,
               cfg->score == MOTE_SCORE_SIGMOID, G, cfg->top_groups, cfg->group_top, cfg->renormalise != 0, cfg->scale,
               topk_idx, topk_w, logits, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};
-  const size_t split = route_split_bytes(T, d, E);
-  const bool may_split = split > 0 && workspace && reinterpret_cast<uintptr_t>(workspace) % kAlign == 0 &&
-                         workspace_bytes >= (stats ? route_workspace_bytes(T, d, E, true) : 0) + split;
   MOTE_HIP(launch_route(a, expert_counts, score_sum, workspace, may_split, static_cast<hipStream_t>(hip_stream)));
   return MOTE_OK;
 }

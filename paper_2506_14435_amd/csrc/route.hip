@@ -948,11 +948,16 @@ size_t route_split_bytes(int T, int d, int E) {
   return shares > 1 ? align256(static_cast<size_t>(route_blocks(T)) * shares * sizeof(RoutePart)) : 0;
 }
 
+size_t route_stats_bytes(int T) { return align256(static_cast<size_t>(route_blocks(T)) * 64 * (sizeof(double) + sizeof(int32_t)) + 1); }
+size_t route_layout_bytes(int T, int d, int E) {
+  return T > kRouteFewTokens ? align256(static_cast<size_t>(d / kRtUnit) * (4 * route_operands(E) * 1024 + 64 * 12) + static_cast<size_t>(E) * d * 2) : 0;
+}
+// A split has fewer shares as the workgroups become more, and there is none above kRouteUnlaidTokens: the largest one of all
+// numbers of tokens up to T.
 size_t route_workspace_bytes(int T, int d, int E, bool stats) {
-  size_t n = 0;
-  if (stats) n += align256(static_cast<size_t>(route_blocks(T)) * 64 * (sizeof(double) + sizeof(int32_t)) + 1);
-  if (T > kRouteFewTokens) n += align256(static_cast<size_t>(d / kRtUnit) * (4 * route_operands(E) * 1024 + 64 * 12) + static_cast<size_t>(E) * d * 2);
-  return n;
+  size_t n = route_layout_bytes(T, d, E);
+  for (int t = kRtTokens; t - kRtTokens < std::min(T, kRouteUnlaidTokens); t += kRtTokens) n = std::max(n, route_split_bytes(t, d, E));
+  return (stats ? route_stats_bytes(T) : 0) + n;
 }
 
 hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* workspace, bool split, hipStream_t stream) {
@@ -962,7 +967,7 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
   if (stats) {
     a.part_sum = reinterpret_cast<double*>(ws);
     a.part_cnt = reinterpret_cast<int32_t*>(a.part_sum + static_cast<int64_t>(blocks) * 64);
-    ws += align256(static_cast<size_t>(blocks) * 64 * (sizeof(double) + sizeof(int32_t)) + 1);
+    ws += route_stats_bytes(a.T);
   }
   // odd E: two experts of a row are two words (3584 x 63 37 us, laid out 19)
   const bool lay = a.T > kRouteUnlaidTokens || (a.T > kRouteFewTokens && !split && (route_shares(a.T, a.d, a.E) > 1 || (a.E > 16 && a.E % 2 != 0)));

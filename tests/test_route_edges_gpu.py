@@ -139,3 +139,15 @@ def test_route_tells_close_logits_of_one_unit_apart(T, E, spread):
     for b in (None, bias):
         for cfg in (dict(), dict(score="sigmoid", renormalise=True), dict(n_groups=8, top_groups=4, group_top=2)):
             _check_route(x, w, b, None, 8, **cfg)
+
+
+@pytest.mark.parametrize("T", [65, 500, 1024])
+def test_route_on_the_workspace_of_a_larger_batch(T):
+    """The same bits whether the workspace is the batch's own or the largest batch's."""
+    g, x, w = _router(T, 3584, 64, T)
+    x, w, r = x.cuda(), w.cuda(), M.MoteRouting(6, renormalise=True)
+    large = torch.empty(M.load_library().mote_route_workspace_bytes(4096, 3584, 64), dtype=torch.uint8, device="cuda")
+    own, shared = M.mote_route(x, w, r, want_logits=True, want_stats=True), M.mote_route(x, w, r, want_logits=True, want_stats=True, workspace=large)
+    torch.cuda.synchronize()
+    for a, b in zip(own, shared):
+        assert torch.equal(a, b)
