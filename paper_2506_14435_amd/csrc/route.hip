@@ -419,7 +419,7 @@ __global__ __launch_bounds__(kLayThreads) void route_layout_kernel(const uint16_
 // fp64 logits of two experts of a token by one wavefront, eight channels of both a lane and round (half a wavefront for each expert,
 // twice the rounds: 16301 x 3584 x 60 72.5 us instead of 69.7).  Code that a workgroup in fifty reaches is fetched from memory when
 // it does (some 1000 cycles for 64 bytes of it, under the stream of the hidden states): here and below it is short rather than unrolled.
-template <bool LAID>
+template <bool COLS>
 __device__ __forceinline__ void settle_two(const RouteArgs& a, int tok, int e0, int e1, double* l_row) {
   const int lane = threadIdx.x & 63;
   const uint16_t* const xr = a.x + static_cast<int64_t>(tok) * a.d;
@@ -428,7 +428,7 @@ __device__ __forceinline__ void settle_two(const RouteArgs& a, int tok, int e0, 
   for (int c = 8 * lane; c < a.d; c += 8 * 64) {
     const u4 x = *reinterpret_cast<const u4*>(xr + c);
     u4 w[2];
-    if constexpr (LAID) {
+    if constexpr (COLS) {
       w[0] = a.cols[(static_cast<int64_t>(e0) * a.d + c) >> 3];
       w[1] = a.cols[(static_cast<int64_t>(e1) * a.d + c) >> 3];
     } else {
@@ -499,10 +499,9 @@ __device__ __forceinline__ float dot2(uint32_t v, float c) {
 // The logits' sums of units [u_lo, u_hi), one set per wavefront, in lds.red (a barrier is still to come), the norms' shares in
 // lds.nx, nw, orx and orw.
 template <int NF, bool LAID, int NL, bool PAIRS>
-__device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, int u_lo, int u_hi) {
+__device__ __forceinline__ void route_logits(const RouteArgs& a, RouteLds& lds, int t0, int u_lo, int u_hi) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int r = lane & 31, g = lane >> 5;
-  const int t0 = blockIdx.x * kRtTokens;
   // neighbouring units go to one wavefront: at any time the eight read places of a row that lie far apart (rows are often a
   // multiple of 4096 bytes, and so are the places of one memory channel)
   const int units = a.d / kRtUnit, u_begin = u_lo + wave * (u_hi - u_lo) / kRtWaves, u_end = u_lo + (wave + 1) * (u_hi - u_lo) / kRtWaves;
@@ -712,7 +711,8 @@ __device__ __forceinline__ void route_start(RouteLds& lds) {
 }
 
 // From the logits (lds.l) to the outputs
-template <bool LAID>
+// LAID: the bound knows the q's; COLS: there are columns of the router's weights
+template <bool LAID, bool COLS>
 __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * kRtTokens;
   // Selection: 16 lanes per token, all 32 at once.
@@ -754,7 +754,7 @@ __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) 
       int* const sel = lds.sel[tq];
       if (st > 0) {
         const int e0 = __builtin_amdgcn_readfirstlane(sel[st - 1]), e1 = __builtin_amdgcn_readfirstlane(sel[st]);
-        settle_two<LAID>(a, t0 + tq, e0, e1, l_row);
+        settle_two<COLS>(a, t0 + tq, e0, e1, l_row);
         if (order_two(a, l_row, sel, st, e0, e1, __shfl(shift, 16 * q, kWave), __shfl(total, 16 * q, kWave), tol_q)) continue;
       }
       uint64_t exact = z ? all : 0, next = tol_q < INFINITY ? 0 : all;
@@ -766,7 +766,7 @@ __device__ __forceinline__ void route_finish(const RouteArgs& a, RouteLds& lds) 
           next &= next - 1;
           const int e1 = next ? __builtin_ctzll(next) : e0;
           if (next) next &= next - 1;
-          settle_two<LAID>(a, t0 + tq, e0, e1, l_row);
+          settle_two<COLS>(a, t0 + tq, e0, e1, l_row);
         }
         next = route_select_exact(a, l_row, lds.pick.key[tq], lds.pick.grp[tq], sel, tol_q, exact);
         if (next == 0) break;
@@ -827,7 +827,7 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
   __shared__ __attribute__((aligned(16))) RouteLds lds;
   const int tid = threadIdx.x, wave = tid >> 6;
   route_start(lds);
-  route_logits<NF, LAID, NL, PAIRS>(a, lds, 0, a.d / kRtUnit);
+  route_logits<NF, LAID, NL, PAIRS>(a, lds, blockIdx.x * kRtTokens, 0, a.d / kRtUnit);
   if (wave == 0) put_w2<LAID>(a, lds, expert_norm<LAID>(lds));
   else if (wave == 1 && (tid & 63) < kRtTokens) put_x2(lds, token_norm<LAID>(lds));
   __syncthreads();
@@ -837,23 +837,39 @@ __global__ __launch_bounds__(kRtThreads) void route_kernel(RouteArgs a) {
     lds.l[token_of(at)][expert_of<NF>(at)] = element_sum(lds, at);
   }
   __syncthreads();
-  route_finish<LAID>(a, lds);
+  route_finish<LAID, LAID>(a, lds);
 }
 
 // Few tokens and many channels: the bytes of the router's rows and of the tokens, at the 30 a cycle that a CU takes in, are
-// what a workgroup's time is made of.  Shares of the channels (blockIdx.y) go to workgroups of their own, which leave their sums
-// and norms in memory, and a second kernel adds them in order and goes on.
+// what a workgroup's time is made of.  Shares of the channels go to workgroups of their own, which leave their sums
+// and norms in memory, and a second kernel adds them in order and goes on.  Workgroups behind those write the weights as columns, from
+// which it settles logits (out of the rows a pair is a line of memory for each channel, at those 30 bytes a cycle: 64 x 3584 x 64 in
+// groups, with a pair to settle 24.5 us, out of columns 19.8; with a border between groups 39 and 30; with nothing to settle 16.2).
 struct RoutePart {
   double l[kRtTokens * 64];        // in the order of lds.red
   float nx[kRtTokens], nw[64];
   uint32_t orx[kRtTokens], orw, unused[31];
 };
 template <int NL, bool PAIRS>
-__global__ __launch_bounds__(kRtThreads) void route_part_kernel(RouteArgs a, RoutePart* __restrict__ parts) {
+__global__ __launch_bounds__(kRtThreads) void route_part_kernel(RouteArgs a, RoutePart* __restrict__ parts, u4* __restrict__ cols, int blocks, int shares) {
   __shared__ __attribute__((aligned(16))) RouteLds lds;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, units = a.d / kRtUnit, share = blockIdx.y, shares = gridDim.y;
-  RoutePart& out = parts[blockIdx.x * shares + share];
-  route_logits<2, false, NL, PAIRS>(a, lds, share * units / shares, (share + 1) * units / shares);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, units = a.d / kRtUnit;
+  const int block = blockIdx.x / shares, share = blockIdx.x - block * shares;
+  if (block >= blocks) {   // eight channels of an expert a thread
+    const int first = static_cast<int>(blockIdx.x) - blocks * shares, step = static_cast<int>(gridDim.x) - blocks * shares;
+    if (lane < a.E)
+      for (int u = first; u < units; u += step) {
+        const int c = u * kRtUnit + 8 * wave;
+        const uint16_t* const p = a.w_router + static_cast<size_t>(c) * a.E + lane;
+        u4 o;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = p[2 * q * a.E] | static_cast<uint32_t>(p[(2 * q + 1) * a.E]) << 16;
+        cols[(static_cast<int64_t>(lane) * a.d + c) >> 3] = o;
+      }
+    return;
+  }
+  RoutePart& out = parts[blockIdx.x];
+  route_logits<2, false, NL, PAIRS>(a, lds, block * kRtTokens, share * units / shares, (share + 1) * units / shares);
   if (wave == 0) {
     const Norms r = expert_norm<false>(lds);
     out.nw[lane] = r.n;
@@ -894,7 +910,7 @@ __global__ __launch_bounds__(kRtThreads) void route_join_kernel(RouteArgs a, con
     lds.l[token_of(at)][expert_of<2>(at)] = sum[i];
   }
   __syncthreads();
-  route_finish<false>(a, lds);
+  route_finish<false, true>(a, lds);
 }
 
 // Counts and score sums of all workgroups in a fixed order: 16 experts per workgroup, 64 slices of the partial sums.
@@ -945,7 +961,7 @@ static int route_shares(int T, int d, int E) {
 }
 size_t route_split_bytes(int T, int d, int E) {
   const int shares = route_shares(T, d, E);
-  return shares > 1 ? align256(static_cast<size_t>(route_blocks(T)) * shares * sizeof(RoutePart)) : 0;
+  return shares > 1 ? align256(static_cast<size_t>(route_blocks(T)) * shares * sizeof(RoutePart)) + align256(static_cast<size_t>(E) * d * 2) : 0;
 }
 
 size_t route_stats_bytes(int T) { return align256(static_cast<size_t>(route_blocks(T)) * 64 * (sizeof(double) + sizeof(int32_t)) + 1); }
@@ -993,11 +1009,13 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
   } else if (split) {
     const int shares = route_shares(a.T, a.d, a.E);
     RoutePart* const parts = reinterpret_cast<RoutePart*>(ws);
-    const dim3 grid(blocks, shares);
-    if (a.E <= 16 && a.E % 2 == 0) route_part_kernel<2, true><<<grid, kRtThreads, 0, stream>>>(a, parts);
-    else if (a.E <= 16) route_part_kernel<2, false><<<grid, kRtThreads, 0, stream>>>(a, parts);
-    else if (a.E % 2 == 0) route_part_kernel<8, true><<<grid, kRtThreads, 0, stream>>>(a, parts);
-    else route_part_kernel<8, false><<<grid, kRtThreads, 0, stream>>>(a, parts);
+    u4* const cols = reinterpret_cast<u4*>(ws + align256(static_cast<size_t>(blocks) * shares * sizeof(RoutePart)));
+    a.cols = cols;
+    const int grid = blocks * shares + std::min(units, std::max(256 - blocks * shares, 16));   // columns on the CUs that are left
+    if (a.E <= 16 && a.E % 2 == 0) route_part_kernel<2, true><<<grid, kRtThreads, 0, stream>>>(a, parts, cols, blocks, shares);
+    else if (a.E <= 16) route_part_kernel<2, false><<<grid, kRtThreads, 0, stream>>>(a, parts, cols, blocks, shares);
+    else if (a.E % 2 == 0) route_part_kernel<8, true><<<grid, kRtThreads, 0, stream>>>(a, parts, cols, blocks, shares);
+    else route_part_kernel<8, false><<<grid, kRtThreads, 0, stream>>>(a, parts, cols, blocks, shares);
     route_join_kernel<<<blocks, kRtThreads, 0, stream>>>(a, parts, shares);
   } else if (a.T > 0) {
     if (a.E <= 16 && a.E % 2 == 0) route_kernel<2, false, 2, true><<<blocks, kRtThreads, 0, stream>>>(a);
