@@ -351,9 +351,9 @@ mote_status mote_layer_forward_static(const mote_layer* layer, const void* x, in
 /* mote_layer_forward on a routing that the caller has, of mote_route or of a scheme of its own, in the place of the
  * layer's router (w_router and router_bias are not read and may be NULL).
  * topk_idx in : int32 [T, k], k = layer->top_k;  topk_w in : fp32 [T, k]
- * A slot whose index is outside 0 .. E - 1 adds nothing to its token (its row is computed, with weight 0, as one of expert
- * 0); an expert twice in a row adds twice.  Everything else, workspace and limits included, as in mote_layer_forward;
- * taps->topk_idx and topk_p are the routing as it was used. */
+ * A slot whose index is outside 0 .. E - 1 has no row and adds nothing to its token; an expert twice in a row adds twice.
+ * Everything else, workspace and limits included, as in mote_layer_forward.  taps->topk_idx, topk_p and row_of are the routing
+ * as it was used, -1, 0 and -1 for such a slot; the taps of dispatch rows end with the rows that there are (the sum of counts). */
 mote_status mote_layer_forward_routed(const mote_layer* layer, const void* x, int T, const int32_t* topk_idx,
                                       const float* topk_w, void* out, void* workspace, size_t workspace_bytes,
                                       const mote_taps* taps, void* hip_stream);

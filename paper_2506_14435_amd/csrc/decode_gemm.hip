@@ -123,7 +123,8 @@ __device__ __forceinline__ void make_local_plan(const RoutedGemmArgs& a, LocalPl
     if (writer && lane < a.E) {
       a.plan.counts[lane] = c;
       a.plan.offsets[lane] = off;
-      if (lane == 0) { a.plan.n_tiles[0] = n_tiles; a.plan.offsets[a.E] = R; }
+      if (lane == 0) a.plan.n_tiles[0] = n_tiles;
+      if (lane == a.E - 1) a.plan.offsets[a.E] = off + c;
     }
   }
   __syncthreads();

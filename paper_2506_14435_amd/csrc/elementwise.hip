@@ -74,6 +74,7 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     if (j < k) {
       const int row = a.row_of[t * k + j];
       const int e = a.topk_idx[t * k + j];
+      if (e < 0) continue;   // a slot without an expert
       const float p = a.topk_p[t * k + j];
       const float sc = (a.beta_h[row] / 127.0f) * a.alpha[e * 3 + 2];
       const int64_t ro = static_cast<int64_t>(row) * d + c0;
@@ -139,8 +140,8 @@ __global__ __launch_bounds__(256) void combine_few_kernel(CombineArgs a) {
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int i = t * k + min(j, k - 1);
-    row[j] = a.row_of[i];
     e[j] = a.topk_idx[i];
+    row[j] = max(a.row_of[i], 0);   // -1: a slot without an expert, whose loads are not used
     p[j] = a.topk_p[i];
   }
   float4 y0[PMAX], y1[PMAX];
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(256) void combine_few_kernel(CombineArgs a) {
   for (int j = 0; j < 2; ++j) {
     const int64_t ro = static_cast<int64_t>(row[j]) * d + c0;
     beta[j] = a.beta_h[row[j]];
-    alpha[j] = a.alpha[e[j] * 3 + 2];
+    alpha[j] = a.alpha[max(e[j], 0) * 3 + 2];
 #pragma unroll
     for (int u = 0; u < PMAX; ++u)
       if (u < a.d_planes) {
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(256) void combine_few_kernel(CombineArgs a) {
     }
 #pragma unroll
   for (int j = 0; j < 2; ++j)
-    if (j < k) {
+    if (j < k && e[j] >= 0) {
       int dsum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
       for (int u = 0; u < PMAX; ++u)

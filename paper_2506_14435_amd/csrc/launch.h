@@ -253,8 +253,8 @@ struct RouteBackwardArgs {
 };
 size_t route_backward_workspace_bytes(int T, int d, int E);
 hipError_t launch_route_backward(RouteBackwardArgs a, void* workspace, hipStream_t stream);
-// A caller's routing as the dispatch plan wants it: indices outside 0 .. E - 1 become expert 0 with weight 0.
-hipError_t launch_route_import(const int32_t* idx, const float* w, int n, int E, int32_t* topk_idx, float* topk_p, hipStream_t stream);
+// A caller's routing as the dispatch plan wants it: indices outside 0 .. E - 1 become -1, with weight 0 and without a row.
+hipError_t launch_route_import(const int32_t* idx, const float* w, int n, int E, int32_t* topk_idx, float* topk_p, int32_t* row_of, hipStream_t stream);
 
 // Residual sum with the norms on both sides of it, and its gradient; kinds are those of launch_norm_rows, 0: none.
 struct ResidualArgs {

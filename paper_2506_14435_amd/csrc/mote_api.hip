@@ -515,7 +515,7 @@ mote_status forward_impl(const mote_layer* layer, const mote_norm* norm, const i
     MOTE_HIP(launch_decode_head(ds, layer->router_bias, static_cast<const uint16_t*>(layer->w_router), E, k, w.topk_idx, w.topk_p,
                                 w.q_x, w.beta_x, w.rs_x, w.h_s, stream));
   else if (route_idx) {
-    MOTE_HIP(launch_route_import(route_idx, route_w, R, E, w.topk_idx, w.topk_p, stream));
+    MOTE_HIP(launch_route_import(route_idx, route_w, R, E, w.topk_idx, w.topk_p, w.row_of, stream));
     MOTE_HIP(launch_quant_rows(xb, T, d, w.q_x, w.beta_x, w.rs_x, stream));
   } else
     MOTE_HIP(launch_router_quant(xb, static_cast<const uint16_t*>(layer->w_router), layer->router_bias, T, d, E, k,

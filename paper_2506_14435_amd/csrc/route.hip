@@ -1027,18 +1027,20 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
   return hipGetLastError();
 }
 
+// A caller's routing for the dispatch plan: what is no expert becomes -1, which the plan and the combine pass over.
 __global__ __launch_bounds__(256) void route_import_kernel(const int32_t* __restrict__ idx, const float* __restrict__ w, int n, int E,
-                                                           int32_t* __restrict__ topk_idx, float* __restrict__ topk_p) {
+                                                           int32_t* __restrict__ topk_idx, float* __restrict__ topk_p, int32_t* __restrict__ row_of) {
   const int i = blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
   const int e = idx[i];
   const bool ok = e >= 0 && e < E;
-  topk_idx[i] = ok ? e : 0;
+  topk_idx[i] = ok ? e : -1;
   topk_p[i] = ok ? w[i] : 0.0f;
+  if (!ok) row_of[i] = -1;
 }
 
-hipError_t launch_route_import(const int32_t* idx, const float* w, int n, int E, int32_t* topk_idx, float* topk_p, hipStream_t stream) {
-  if (n > 0) route_import_kernel<<<(n + 255) / 256, 256, 0, stream>>>(idx, w, n, E, topk_idx, topk_p);
+hipError_t launch_route_import(const int32_t* idx, const float* w, int n, int E, int32_t* topk_idx, float* topk_p, int32_t* row_of, hipStream_t stream) {
+  if (n > 0) route_import_kernel<<<(n + 255) / 256, 256, 0, stream>>>(idx, w, n, E, topk_idx, topk_p, row_of);
   return hipGetLastError();
 }
 

@@ -266,7 +266,10 @@ __global__ __launch_bounds__(kPlanThreads) void dispatch_plan_kernel(const int32
 #pragma unroll
   for (int j = 0; j < kItems; ++j)
     if (first[j] >= 0) atomicAdd(&s_cnt[first[j]], 1);
-  for (int i = kPass + tid; i < R; i += kPlanThreads) atomicAdd(&s_cnt[topk_idx[i]], 1);
+  for (int i = kPass + tid; i < R; i += kPlanThreads) {
+    const int v = topk_idx[i];
+    if (v >= 0) atomicAdd(&s_cnt[v], 1);          // -1: a slot without an expert (given routings only)
+  }
   __syncthreads();
   if (tid == 0) {
     int off = 0, tiles = 0;
