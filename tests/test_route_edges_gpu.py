@@ -151,3 +151,28 @@ def test_route_on_the_workspace_of_a_larger_batch(T):
     torch.cuda.synchronize()
     for a, b in zip(own, shared):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [40, 1060])
+@pytest.mark.parametrize("renormalise", [False, True])
+def test_weights_of_large_logits_keep_their_bits(T, renormalise):
+    """Logits of one product each, exact in fp32 and far from zero: what is left are the roundings of the weight itself.  In units of
+    2^-24 of it: exp2 2 and its argument 1, the sum with 1 and the quotient 1 each, the scale 1 (6); renormalised, log 2 and the sum in
+    it 1 (absolute: s near 0 or 1), exp2 and its argument 3, the sum of four terms 2, quotient and scale 1 each (10)."""
+    g = torch.Generator().manual_seed(T)
+    x, w = torch.zeros(T, 128), torch.zeros(128, 12)
+    x[:, 3] = 1 + torch.randint(0, 128, (T,), generator=g) / 128
+    w[3] = -24 - torch.arange(12) * 0.75
+    w[3, 6:] *= -1 if renormalise else 1                               # of both signs: some scores are 1 less nothing
+    x, w = x.to(torch.bfloat16), w.to(torch.bfloat16)
+    bias = torch.zeros(12)
+    bias[[1, 4, 8, 11]] = 2.0                                          # chosen whatever their scores
+    for score in ("sigmoid", "softmax"):
+        ref = O.route(_np(x), _np(w), 4, score, select_bias=bias.numpy(), renormalise=renormalise, scale=2.5)
+        r = M.mote_route(x.cuda(), w.cuda(), M.MoteRouting(4, score=score, renormalise=renormalise, scale=2.5), select_bias=bias.cuda())
+        torch.cuda.synchronize()
+        assert np.array_equal(r.topk_idx.cpu().numpy(), ref["idx"])
+        err = np.abs(_np(r.topk_w) - ref["w"])
+        # a softmax weight that is not renormalised is divided by the fp32 sum of 12 exponentials: 22 more with the roundings of theirs
+        units = 10 if renormalise else 6 if score == "sigmoid" else 28
+        assert (err <= units * 2.0 ** -24 * ref["w"] + 1e-37).all(), (err / ref["w"]).max() * 2 ** 24
