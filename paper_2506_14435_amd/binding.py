@@ -518,8 +518,12 @@ class MoteRouting:
                  renormalise: bool = False, scale: float = 1.0):
         if score not in SCORES:
             raise MoteError(f"score must be one of {SCORES}, got {score!r}")
-        self.top_k = int(top_k)
-        self.struct = MoteRoutingStruct(SCORES.index(score), self.top_k, n_groups, top_groups, group_top, 1 if renormalise else 0, scale)
+        self.struct = MoteRoutingStruct(SCORES.index(score), int(top_k), n_groups, top_groups, group_top, 1 if renormalise else 0, scale)
+
+    @property
+    def top_k(self) -> int:
+        """Slots of a token.  Read-only, and the struct's own: the outputs are allocated by it and the kernels write by it."""
+        return self.struct.top_k
 
 
 class Routed(NamedTuple):
@@ -608,7 +612,7 @@ class MoteResidual:
 
     def __init__(self, d: int, post: MoteNorm = None, gate: torch.Tensor = None, pre: MoteNorm = None,
                  residual_scale: float = 1.0, branch_scale: float = 1.0):
-        self.d, self.post, self.gate, self.pre = int(d), post, gate, pre
+        self._d, self.post, self.gate, self.pre = int(d), post, gate, pre
         for name, t in (("post gamma", post and post.gamma), ("gate", gate), ("pre gamma", pre and pre.gamma)):
             if t is not None:
                 _shape(_dev(t, torch.bfloat16, name), (self.d,), name)
@@ -619,6 +623,11 @@ class MoteResidual:
         params = [p for p in (gate, post and post.gamma, post and post.beta, pre and pre.gamma, pre and pre.beta) if p is not None]
         _one_device(**{f"parameter {i}": p for i, p in enumerate(params)})
         self._param = params[0] if params else None   # says where the parameters are
+
+    @property
+    def d(self) -> int:
+        """Width of a row.  Read-only: the parameters have it."""
+        return self._d
 
 
 def _residual_operands(block: MoteResidual, **tensors):

@@ -59,3 +59,14 @@ def test_route_workspace_below_the_least_is_refused(lib):
         assert _call(lib, T, d, E, 256, 512) == 3 and _call(lib, T, d, E, None, 1 << 30) == 1 and _call(lib, T, d, E, 128, 1 << 30) == 1
         assert _call(lib, T, d, E, 256, 1024, counts=256) == 3
     assert _call(lib, 4, 256, 8, 256, 16, counts=256) == 3
+
+
+def test_sizes_of_a_description_do_not_part_from_what_the_kernels_write():
+    """Outputs are allocated by top_k and d, kernels write by the struct and read the parameters: neither can be set on its own."""
+    r, block = M.MoteRouting(2), M.MoteResidual(256)
+    assert r.top_k == 2 and block.d == 256
+    for obj, name in ((r, "top_k"), (block, "d")):
+        with pytest.raises(AttributeError):
+            setattr(obj, name, 4)
+    r.struct.top_k = 3
+    assert r.top_k == 3
