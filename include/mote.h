@@ -231,7 +231,9 @@ mote_status mote_route(const mote_routing* cfg, const void* x, const void* w_rou
  *   dlogits = d(sum_tj d_topk_w[t,j] * topk_w[t,j] + sum_e d_score_sum[e] * score_sum[e]) / dlogits      (fp32)
  *   dx[t,c] = sum_e dlogits[t,e] * w_router[c,e],     dw_router[c,e] = sum_t x[t,c] * dlogits[t,e]
  *
- * d_score_sum of Eq.12 with weight gamma is gamma * E / T * expert_counts (counts are constants there too).
+ * d_score_sum of Eq.12 with weight gamma is gamma * E / T * expert_counts (counts are constants there too).  d_topk_w is the
+ * caller's: for the layer's sum the product of dL/dout[t] with the output of slot j's expert.  Losses on the logits themselves have
+ * no part here: their dlogits go into dx and dw_router by the two products above, added by the caller.
  * Operands of the two products are exact (fp32 dlogits as three bf16 terms against bf16 x and w_router), sums are fp32 in a
  * fixed order.  A padding token (token_mask) has a zero gradient row (finite w_router); slots of index -1 have no part.
  *
@@ -406,7 +408,8 @@ mote_status mote_residual_norm_backward(const mote_residual* block, const void* 
  *   norm = sqrt(sum over all tensors and elements of g^2)        (fp64 sums in a fixed order)
  *   out  = g * c (fp64, rounded to fp32 and then to the type), c = max_norm / norm where norm > max_norm, else 1
  *
- * A norm that is not finite leaves the values as they are (c = 1) and is reported, so that the caller can skip the step.
+ * A norm that is not finite leaves the values as they are (c = 1) and is reported, so that the caller can skip the step.  A
+ * finite one beyond fp32 (above 3.4e38) clips as any other and is reported as +inf.
  * grads_host in : HOST array of n descriptors, read before the call returns.  out == NULL or out == grad: in place, not
  *                 written where c == 1.  Tensors of zero elements are allowed.  Pointers need the alignment of their type
  *                 only (16 bytes are faster).  No two outputs may overlap, nor an output another tensor's gradient: such a

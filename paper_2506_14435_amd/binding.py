@@ -577,7 +577,9 @@ def mote_route_backward(x: torch.Tensor, w_router: torch.Tensor, routing: MoteRo
                         topk_idx: torch.Tensor, d_topk_w: torch.Tensor, d_score_sum: torch.Tensor = None,
                         token_mask: torch.Tensor = None, want_dx: bool = True, want_dw: bool = True,
                         workspace: torch.Tensor = None):
-    """Gradients of mote_route: (dx fp32 [T, d], dw_router fp32 [d, E]) for d_topk_w fp32 [T, k] and d_score_sum fp32 [E]."""
+    """Gradients of mote_route: (dx fp32 [T, d], dw_router fp32 [d, E]) for d_topk_w fp32 [T, k] and d_score_sum fp32 [E].
+    d_topk_w is the caller's (of the layer's sum: dL/dout of the token times the output of the slot's expert); gradients of the
+    logits themselves are not taken."""
     n_tok, d, n_exp, token_mask = _router_operands(x, w_router, token_mask)
     _shape(_dev(logits, torch.float32, "logits"), (n_tok, n_exp), "logits")
     _shape(_dev(topk_idx, torch.int32, "topk_idx"), (n_tok, routing.top_k), "topk_idx")
@@ -686,7 +688,10 @@ def mote_residual_norm_backward(block: MoteResidual, r: torch.Tensor, y: torch.T
 
 class GradClip:
     """The list of gradients (contiguous fp32 or bf16 device tensors of one device) that mote_clip_grad_norm measures and
-    scales, in place or into `outs` (one per gradient, None: in place), with its descriptors and workspace."""
+    scales, in place or into `outs` (one per gradient, None: in place), with its descriptors and workspace.
+
+    It holds these tensors, not the parameters they are the gradients of: where a training step puts new tensors in their place
+    (zero_grad with set_to_none), it makes a new GradClip of them; an old one goes on clipping the old tensors."""
 
     def __init__(self, grads, outs=None):
         self.grads = list(grads)
