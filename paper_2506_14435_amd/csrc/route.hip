@@ -477,6 +477,7 @@ __device__ __forceinline__ bool order_two(const RouteArgs& a, const double* l_ro
     score = a.sigmoid ? 1.0 / (1.0 + score) : score / static_cast<double>(total);
     key = score;
     if (a.bias) key += static_cast<double>(a.bias[e]);
+    if (key != key) key = -DBL_MAX;
   }
   const double other = __shfl(key, 1, kWave), apart = fabs(score - __shfl(score, 1, kWave));
   const float part = a.sigmoid || keys_are_logits(a) ? 0.0f : (tol < 0.05f ? 1.1f * tol + 32 * 0x1p-24f : INFINITY);
@@ -954,13 +955,14 @@ static size_t align256(size_t v) { return (v + 255) & ~size_t{255}; }
 static int route_operands(int E) { return E <= 32 ? 1 : 2; }
 
 // Up to this many tokens the workgroups are too few for the chip, and weights that are laid out first come too late: their kernel
-// takes longer than it saves.  One kernel, or split, and laid out first, in us, 128 tokens: 896 x 8 8.9, 9.8; 2048 x 16 11.4, 11.8;
-// 2048 x 64 12.4, 15.0; 3584 x 64 13.8, 19.5; 1024 tokens: 9.1, 10.0; 11.6, 12.1; 17.3, 19.3; 28.1, 29.9; 2048 x 3584 x 64 27.7, 25.2.
+// takes longer than it saves.  One kernel, or split, and laid out first, in us, 128 tokens: 896 x 8 8.9, 10.7; 2048 x 16 11.5, 12.9;
+// 2048 x 64 13.5, 16.4; 3584 x 64 17.1, 21.8; 1024 tokens: 9.7, 11.1; 12.0, 14.1; 17.6, 19.5; 21.6, 24.6; 2048 tokens: 2048 x 64 19.9,
+// 19.4, 3584 x 64 25.2, 24.8 (but 1500 x 896 x 8 9.8, 11.9).
 constexpr int kRouteUnlaidTokens = 1024;
 // Shares of the channels: a unit for each wavefront, 16 at most (d = 16384, E = 64: 16 shares 18.7 us, 32 of them 24.4), a workgroup
 // per CU at most, from 256 KB of operands for a workgroup of 32 tokens on (below, the second launch takes what it saves).  One
-// workgroup, and split, in us: d = 1280, E = 64 12.3, 12.8; 2048 x 64 14.1, 12.3; 3584 x 64 19.1, 14.0; 7168 x 64 30.0, 16.9;
-// 2048 x 32 13.5, 11.7; 4096 x 16 16.3, 12.5; 1024 x 8 8.6, 9.9.
+// workgroup, and split, in us: d = 1280, E = 64 12.1, 12.9; 2048 x 64 14.5, 13.0; 3584 x 64 19.9, 14.8; 7168 x 64 32.7, 19.1;
+// 2048 x 32 13.0, 12.0; 4096 x 16 16.0, 13.3; 1024 x 8 8.8, 10.3.
 static int route_shares(int T, int d, int E) {
   if (T == 0 || T > kRouteUnlaidTokens || d * (kRtTokens + E) < 1 << 17) return 1;
   return std::min({d / (kRtUnit * kRtWaves), 16, 256 / route_blocks(T)});
@@ -991,7 +993,7 @@ hipError_t launch_route(RouteArgs a, int32_t* counts, float* score_sum, void* wo
     a.part_cnt = reinterpret_cast<int32_t*>(a.part_sum + static_cast<int64_t>(blocks) * 64);
     ws += route_stats_bytes(a.T);
   }
-  // odd E: two experts of a row are two words (3584 x 63 37 us, laid out 19)
+  // odd E: two experts of a row are two words (64 x 3584 x 63 in one workgroup for 32 tokens 42 us, 128 tokens laid out 22)
   const bool lay = a.T > kRouteUnlaidTokens || (a.T > kRouteFewTokens && !split && (route_shares(a.T, a.d, a.E) > 1 || (a.E > 16 && a.E % 2 != 0)));
   if (lay) {
     const int nf = route_operands(a.E);

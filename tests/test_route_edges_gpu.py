@@ -176,3 +176,21 @@ def test_weights_of_large_logits_keep_their_bits(T, renormalise):
         # a softmax weight that is not renormalised is divided by the fp32 sum of 12 exponentials: 22 more with the roundings of theirs
         units = 10 if renormalise else 6 if score == "sigmoid" else 28
         assert (err <= units * 2.0 ** -24 * ref["w"] + 1e-37).all(), (err / ref["w"]).max() * 2 ** 24
+
+
+@pytest.mark.parametrize("T", [33, 1060])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_experts_whose_bias_is_not_a_number(T, score):
+    """They rank as the lowest finite value: behind a bias of that value, among themselves by index, wherever they sit."""
+    g, x, w = _router(T, 256, 40, 31)
+    lowest = torch.finfo(torch.float32).min
+    for values, want in (({4: math.nan, 20: math.nan}, [4, 20, -1]), ({4: math.nan, 20: lowest}, [20, 4, -1]), ({4: lowest, 20: math.nan}, [4, 20, -1]),
+                         ({3: 0.0, 9: math.nan, 25: math.nan}, [3, 9, 25]), ({5: math.inf, 21: math.inf, 6: math.nan}, [5, 21, 6]),
+                         ({7: math.nan, 8: math.nan, 39: math.nan}, [7, 8, 39])):
+        bias = torch.full((40,), -math.inf)
+        for e, v in values.items():
+            bias[e] = v
+        r = M.mote_route(x.cuda(), w.cuda(), M.MoteRouting(3, score=score), select_bias=bias.cuda())
+        torch.cuda.synchronize()
+        assert (r.topk_idx.cpu() == torch.tensor(want, dtype=torch.int32)).all(), (values, r.topk_idx[0])
+        assert np.array_equal(O.route(_np(x), _np(w), 3, score, select_bias=bias.numpy())["idx"], r.topk_idx.cpu().numpy())
