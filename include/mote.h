@@ -367,7 +367,8 @@ mote_status mote_layer_forward_routed(const mote_layer* layer, const void* x, in
  *   total  = residual_scale * r + branch_scale * gate * z    (gate == NULL: 1; per channel)
  *   normed = N_pre(total)                                    (pre == NULL: not written)
  *
- * N is the norm of mote_block_forward.  Everything between the loads and the two stores is fp32 (row sums included); normed
+ * N is the norm of mote_block_forward.  Everything between the loads and the two stores is fp32 (row sums included: a row
+ * whose squares add up to more than fp32 holds, values of 1e18 and above, is beyond it, and eps below 1e-45 is 0); normed
  * is taken from the sum before its rounding.
  * dtype        : MOTE_DTYPE_BF16 or MOTE_DTYPE_F32, of r, y, total, normed and their gradients; gamma, beta, gate: bf16 [d]
  * r, y     in  : [T, d];   total, normed out : [T, d]; each may be r or y itself (a row is loaded
